@@ -244,6 +244,105 @@ int gtopk_dense_topk(const float* dense, int64_t m, int32_t k, uint32_t* g_idx, 
                      void* ws, size_t ws_bytes, void* stream);
 
 /*
+ * ---- Before the hot path: a layer in 8 bits (Algorithm 4 lines 2-3, where the gradients come from) ----
+ *
+ * P workers on one GPU hold P sets of activations from the forward pass to the backward pass, and the weight
+ * gradients of the backward pass are the rows that gtopk_step takes.  The calls below keep the
+ * activations packed to 8 bits (activation checkpoints), multiply packed matrices for the forward pass and the input
+ * gradient, and compute every worker's weight gradient from the packed activations into its gradient row.
+ *
+ * A packed matrix of `rows` x `cols` values has, per row and block of 128 columns, 128 codes and one scale:
+ *   codes  [rows][code_stride]  e4m3 (1 sign, 4 exponent, 3 mantissa bits; bias 7; largest 448; 0x7f and 0xff NaN).
+ *                               code_stride: a multiple of 128, >= cols.  The codes from cols up to the
+ *                               end of the last block are 0 (the pack calls write them); what lies behind that block in
+ *                               a row is neither read nor written.
+ *   scales [rows][scale_stride] e8m0: a byte s stands for 2^(s - 127), 255 for NaN.  scale_stride: a multiple of 4,
+ *                               >= ceil(cols / 128); the bytes behind the last block's are not written, and what they hold
+ *                               does not matter (they may be read, up to the next multiple of 4).
+ *   The value of a code c in a block of scale s is e4m3(c) * 2^(s - 127).  codes is 16-byte aligned, scales 4-byte.
+ * Dense matrices (x, dy, out, dx, grad) have contiguous rows at any stride >= their columns and need the
+ * alignment of one value only, as a layer may lie anywhere in a flat row.  dtype is one of gtopk_dtype.
+ * Sizes: rows and columns 1 .. 2^31 - 1; rows (M of the product) may also be 0: then there is nothing to
+ * pack, unpack or multiply, and a weight gradient is 0.  NaN and Inf are allowed as the calls state, unlike in the
+ * calls above.
+ */
+typedef enum { GTOPK_F32 = 0, GTOPK_BF16 = 1, GTOPK_F16 = 2 } gtopk_dtype;
+
+/* f(x) and its derivative f'(x): x; max(x, 0), f'(0) = 0; tanh x; s(x) = 1 / (1 + e^-x); x s(x); x Phi(x) with the normal
+ * distribution function Phi (not its tanh approximation).  Computed in fp32. */
+typedef enum {
+    GTOPK_ACT_NONE = 0, GTOPK_ACT_RELU = 1, GTOPK_ACT_TANH = 2, GTOPK_ACT_SIGMOID = 3, GTOPK_ACT_SILU = 4, GTOPK_ACT_GELU = 5
+} gtopk_act;
+
+/*
+ * Pack a matrix with one scale per row and block of 128 columns (activations, output gradients).
+ * e is the smallest integer with max |x| <= 448 * 2^e over the block's finite values, at least -127 (also for a
+ * block of zeros); the scale is e + 127, a code the e4m3 number nearest to x * 2^-e (ties to
+ * even).  Values that are not finite get the code 0xff (NaN).  Needs no workspace.
+ */
+int gtopk_pack_rows(const void* x, int32_t dtype, int64_t rows, int64_t cols, int64_t stride,
+                    uint8_t* codes, int64_t code_stride, uint8_t* scales, int64_t scale_stride, void* stream);
+
+/*
+ * Pack a matrix with one scale per tile of 128 x 128 (weights), as it is (codes, scales: rows x cols) and / or
+ * transposed (codes_t, scales_t: cols x rows).  Both are packed matrices as above: a tile's scale stands in
+ * each of its rows.  Transposed weights serve the input gradient's product.  Either pair may be NULL, not
+ * both.  e and the codes as in gtopk_pack_rows, with the maximum over the tile.  Needs no workspace.
+ */
+int gtopk_pack_tiles(const void* x, int32_t dtype, int64_t rows, int64_t cols, int64_t stride,
+                     uint8_t* codes, int64_t code_stride, uint8_t* scales, int64_t scale_stride,
+                     uint8_t* codes_t, int64_t code_t_stride, uint8_t* scales_t, int64_t scale_t_stride, void* stream);
+
+/*
+ * out = f(x) with x from a packed matrix, rounded once to dtype: a layer's input recomputed from the checkpoint of what
+ * went into the activation.  With GTOPK_ACT_NONE the values themselves.  Needs no workspace.
+ */
+int gtopk_unpack(const uint8_t* codes, int64_t code_stride, const uint8_t* scales, int64_t scale_stride,
+                 int64_t rows, int64_t cols, int32_t act, void* out, int32_t dtype, int64_t out_stride, void* stream);
+
+/*
+ * dx = dy * f'(x) with x from a packed matrix: the backward pass of an activation from its checkpoint.  dy and dx have the
+ * same dtype; the product is rounded once.  dx may be dy (same pointer, same stride).  A NaN in x gives a NaN.
+ * Needs no workspace.
+ */
+int gtopk_activation_grad(const uint8_t* codes, int64_t code_stride, const uint8_t* scales, int64_t scale_stride,
+                          int64_t rows, int64_t cols, int32_t act, const void* dy, int64_t dy_stride,
+                          void* dx, int64_t dx_stride, int32_t dtype, void* stream);
+
+/*
+ * out = A B^T for packed A (M x K) and packed B (N x K): out[m][n] = sum over k of A[m][k] * B[n][k].  Products are
+ * exact, sums are fp32, the result is rounded once to dtype.  Forward pass of a layer: A its packed input, B its
+ * packed weights; input gradient: A the packed output gradient, B the transposed packed weights.
+ *   ws : gtopk_product_workspace_bytes(M, N, K) bytes (0 if the sizes are invalid)
+ */
+size_t gtopk_product_workspace_bytes(int64_t M, int64_t N, int64_t K);
+int gtopk_scaled_product(const uint8_t* a_codes, int64_t a_code_stride, const uint8_t* a_scales, int64_t a_scale_stride,
+                         const uint8_t* b_codes, int64_t b_code_stride, const uint8_t* b_scales, int64_t b_scale_stride,
+                         int64_t M, int64_t N, int64_t K, void* out, int32_t dtype, int64_t out_stride,
+                         void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Weight gradients of P workers, into their gradient rows: for every worker w, with t over its rows,
+ *     grad[w*grad_stride + n*K + k]  =  (or +=, accumulate != 0)  sum over t of dY[t][n] * X[t][k]
+ *   dy      [rows][dy_stride] : the output gradients of all workers' samples, N columns
+ *   codes, scales             : the packed inputs X of the same samples, K columns (the checkpoint)
+ *   row_begin [P+1]           : device memory; worker w has the rows row_begin[w] .. row_begin[w+1] - 1 (ascending, within
+ *                               0 .. rows; out-of-range entries are clamped, rows that no worker has are left out, a
+ *                               worker without rows gets 0).  NULL: rows / P each, and rows must be a multiple of P
+ *   grad                      : this layer's first weight in worker 0's gradient row; nothing outside the P x N x K
+ *                               values is touched
+ *   P : 1 .. 32768;  grad_stride : >= N*K if P > 1 (the row length m of the step)
+ *   ws : gtopk_weight_grad_workspace_bytes(rows, P, N, K) bytes (0 if the sizes are invalid)
+ * Sums are fp32, in an order that depends on the arguments only; dY enters exactly, whatever its type (an fp16 or fp32
+ * value as a sum of two or three bf16 numbers), but for parts below 2^-126, which may be taken as 0.
+ */
+size_t gtopk_weight_grad_workspace_bytes(int64_t rows, int32_t P, int64_t N, int64_t K);
+int gtopk_weight_grad(const void* dy, int32_t dtype, int64_t dy_stride, const uint8_t* codes, int64_t code_stride,
+                      const uint8_t* scales, int64_t scale_stride, int64_t rows, const int32_t* row_begin, int32_t P,
+                      int64_t N, int64_t K, float* grad, int64_t grad_stride, int32_t accumulate,
+                      void* ws, size_t ws_bytes, void* stream);
+
+/*
  * Instrumentation for benchmarks (not part of the method): gtopk_step with HIP event
  * records at its stage boundaries.  `events` holds the HOST handles of six hipEvent_t
  * (created by the caller, passed as void*), recorded on `stream`:

@@ -24,6 +24,9 @@ EXPORTS = (
     "gtopk_allreduce_workspace_bytes", "gtopk_topk_allreduce", "gtopk_dense_topk",
     "gtopk_step_timed", "gtopk_probe_stream", "gtopk_debug_candidate_counts", "gtopk_debug_plan",
     "gtopk_debug_merge_kept", "gtopk_debug_routes", "gtopk_debug_missed_brackets",
+    "gtopk_pack_rows", "gtopk_pack_tiles", "gtopk_unpack", "gtopk_activation_grad",
+    "gtopk_product_workspace_bytes", "gtopk_scaled_product",
+    "gtopk_weight_grad_workspace_bytes", "gtopk_weight_grad",
 )
 
 GTOPK_OK, GTOPK_EINVAL, GTOPK_EWORKSPACE, GTOPK_EALIGN, GTOPK_EHIP = 0, -1, -2, -3, -4
@@ -97,6 +100,22 @@ def load() -> ctypes.CDLL:
     lib.gtopk_debug_candidate_counts.restype = c.c_int
     lib.gtopk_debug_candidate_counts.argtypes = [vp, i64, i32, i32, c.POINTER(c.c_uint32),
                                                  c.POINTER(c.c_uint32)]
+    lib.gtopk_pack_rows.restype = c.c_int
+    lib.gtopk_pack_rows.argtypes = [vp, i32, i64, i64, i64, vp, i64, vp, i64, vp]
+    lib.gtopk_pack_tiles.restype = c.c_int
+    lib.gtopk_pack_tiles.argtypes = [vp, i32, i64, i64, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp]
+    lib.gtopk_unpack.restype = c.c_int
+    lib.gtopk_unpack.argtypes = [vp, i64, vp, i64, i64, i64, i32, vp, i32, i64, vp]
+    lib.gtopk_activation_grad.restype = c.c_int
+    lib.gtopk_activation_grad.argtypes = [vp, i64, vp, i64, i64, i64, i32, vp, i64, vp, i64, i32, vp]
+    lib.gtopk_product_workspace_bytes.restype = sz
+    lib.gtopk_product_workspace_bytes.argtypes = [i64, i64, i64]
+    lib.gtopk_scaled_product.restype = c.c_int
+    lib.gtopk_scaled_product.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, i64, i64, i64, vp, i32, i64, vp, sz, vp]
+    lib.gtopk_weight_grad_workspace_bytes.restype = sz
+    lib.gtopk_weight_grad_workspace_bytes.argtypes = [i64, i32, i64, i64]
+    lib.gtopk_weight_grad.restype = c.c_int
+    lib.gtopk_weight_grad.argtypes = [vp, i32, i64, vp, i64, vp, i64, i64, vp, i32, i64, i64, vp, i64, i32, vp, sz, vp]
     _lib = lib
     return lib
 
@@ -407,3 +426,185 @@ def gtopk_debug_candidate_counts(ws, m: int, k: int, P: int):
                                              ctypes.byref(cap))
     _check(rc, "gtopk_debug_candidate_counts")
     return list(counts), int(cap.value)
+
+
+# -- a layer in 8 bits ----------------------------------------------------------
+# codes and scales are torch.uint8 tensors ([rows][code_stride], [rows][scale_stride]; alloc_packed makes them);
+# dense matrices are 2-D float32, bfloat16 or float16 tensors with contiguous rows.  All tensors of a call lie on one
+# GPU, and the call runs there, on that GPU's current stream.
+
+ACTS = ("none", "relu", "tanh", "sigmoid", "silu", "gelu")
+PACK_BLOCK = 128
+
+
+def _dtype_code(t, name: str) -> int:
+    torch = _torch()
+    codes = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+    if not isinstance(t, torch.Tensor) or t.dtype not in codes:
+        raise TypeError(f"{name} must be a float32, bfloat16 or float16 tensor")
+    return codes[t.dtype]
+
+
+def _act_code(act: str) -> int:
+    if act not in ACTS:
+        raise ValueError(f"act must be one of {ACTS}, got {act!r}")
+    return ACTS.index(act)
+
+
+def _dense(t, name: str):
+    """(rows, cols, stride) of a dense 2-D matrix with contiguous rows."""
+    if t.dim() != 2 or t.shape[1] < 1 or (t.stride(1) != 1 and t.shape[1] > 1):
+        raise ValueError(f"{name} must be 2-D with contiguous rows")
+    return t.shape[0], t.shape[1], (t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1]))
+
+
+def _packed(codes, scales, rows: int, cols: int, name: str):
+    """(code_stride, scale_stride) of the packed matrix `name` that must hold rows x cols values."""
+    nb = -(-cols // PACK_BLOCK)
+    for t, least, of, what in ((codes, nb * PACK_BLOCK, PACK_BLOCK, "codes"), (scales, nb, 4, "scales")):
+        if t.dim() != 2 or t.shape[0] != rows or t.shape[1] < least or (t.stride(1) != 1 and t.shape[1] > 1):
+            raise ValueError(f"{name}{what} must be 2-D with contiguous rows, {rows} rows of at least {least} bytes")
+        # the last row is read to its multiple, so it must be there
+        if t.shape[1] % of:
+            raise ValueError(f"{name}{what} must have a multiple of {of} columns")
+    stride = lambda t: t.stride(0) if rows > 1 else t.shape[1]
+    return stride(codes), stride(scales)
+
+
+def _on_device(*tensors):
+    """A context in which the tensors' GPU is the current one; ValueError if they lie on several."""
+    torch = _torch()
+    devices = {t.device for t in tensors if isinstance(t, torch.Tensor)}
+    if len(devices) > 1:
+        raise ValueError(f"tensors lie on several devices: {sorted(map(str, devices))}")
+    return torch.cuda.device(devices.pop())
+
+
+def alloc_packed(rows: int, cols: int, device="cuda"):
+    """(codes, scales) of a packed matrix of rows x cols values, for the pack calls to fill."""
+    torch = _torch()
+    nb = -(-cols // PACK_BLOCK)
+    return (torch.empty((rows, nb * PACK_BLOCK), dtype=torch.uint8, device=device),
+            torch.empty((rows, -(-nb // 4) * 4), dtype=torch.uint8, device=device))
+
+
+def gtopk_pack_rows(x, codes, scales) -> None:
+    torch = _torch()
+    dtype = _dtype_code(x, "x")
+    rows, cols, stride = _dense(x, "x")
+    px, pc, ps = _ptr(x, x.dtype, "x"), _ptr(codes, torch.uint8, "codes"), _ptr(scales, torch.uint8, "scales")
+    code_stride, scale_stride = _packed(codes, scales, rows, cols, "")
+    with _on_device(x, codes, scales):
+        rc = load().gtopk_pack_rows(px, dtype, rows, cols, stride, pc, code_stride, ps, scale_stride, _stream())
+    _check(rc, "gtopk_pack_rows")
+
+
+def gtopk_pack_tiles(x, codes=None, scales=None, codes_t=None, scales_t=None) -> None:
+    """Either pair may be None, not both."""
+    torch = _torch()
+    dtype = _dtype_code(x, "x")
+    rows, cols, stride = _dense(x, "x")
+    args = [_ptr(x, x.dtype, "x"), dtype, rows, cols, stride]
+    for c, s, shape, name in ((codes, scales, (rows, cols), ""), (codes_t, scales_t, (cols, rows), "transposed ")):
+        if (c is None) != (s is None):
+            raise ValueError(f"{name}codes and scales go together")
+        pc, ps = _ptr(c, torch.uint8, name + "codes", True), _ptr(s, torch.uint8, name + "scales", True)
+        if c is None or rows == 0:
+            args += [pc, 0, ps, 0]
+        else:
+            code_stride, scale_stride = _packed(c, s, *shape, name)
+            args += [pc, code_stride, ps, scale_stride]
+    with _on_device(x, codes, scales, codes_t, scales_t):
+        rc = load().gtopk_pack_tiles(*args, _stream())
+    _check(rc, "gtopk_pack_tiles")
+
+
+def gtopk_unpack(codes, scales, act: str, out) -> None:
+    torch = _torch()
+    dtype = _dtype_code(out, "out")
+    rows, cols, stride = _dense(out, "out")
+    pc, ps, po = _ptr(codes, torch.uint8, "codes"), _ptr(scales, torch.uint8, "scales"), _ptr(out, out.dtype, "out")
+    code_stride, scale_stride = _packed(codes, scales, rows, cols, "")
+    with _on_device(codes, scales, out):
+        rc = load().gtopk_unpack(pc, code_stride, ps, scale_stride, rows, cols, _act_code(act), po, dtype, stride, _stream())
+    _check(rc, "gtopk_unpack")
+
+
+def gtopk_activation_grad(codes, scales, act: str, dy, dx) -> None:
+    """dx may be dy."""
+    torch = _torch()
+    dtype = _dtype_code(dy, "dy")
+    rows, cols, dy_stride = _dense(dy, "dy")
+    if _dense(dx, "dx")[:2] != (rows, cols):
+        raise ValueError("dy and dx must have the same shape")
+    pc, ps = _ptr(codes, torch.uint8, "codes"), _ptr(scales, torch.uint8, "scales")
+    pd, px = _ptr(dy, dy.dtype, "dy"), _ptr(dx, dy.dtype, "dx")
+    code_stride, scale_stride = _packed(codes, scales, rows, cols, "")
+    with _on_device(codes, scales, dy, dx):
+        rc = load().gtopk_activation_grad(pc, code_stride, ps, scale_stride, rows, cols, _act_code(act), pd, dy_stride, px,
+                                          _dense(dx, "dx")[2], dtype, _stream())
+    _check(rc, "gtopk_activation_grad")
+
+
+def gtopk_product_workspace_bytes(M: int, N: int, K: int) -> int:
+    return int(load().gtopk_product_workspace_bytes(M, N, K))
+
+
+def alloc_product_workspace(M: int, N: int, K: int, device="cuda"):
+    torch = _torch()
+    n = gtopk_product_workspace_bytes(M, N, K)
+    if n == 0:
+        raise GtopkError(GTOPK_EINVAL, "gtopk_product_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def gtopk_scaled_product(a_codes, a_scales, b_codes, b_scales, K: int, out, ws) -> None:
+    """out [M][N] = A B^T for packed A (M x K) and B (N x K)."""
+    torch = _torch()
+    dtype = _dtype_code(out, "out")
+    M, N, stride = _dense(out, "out")
+    pa, pas = _ptr(a_codes, torch.uint8, "a_codes"), _ptr(a_scales, torch.uint8, "a_scales")
+    pb, pbs = _ptr(b_codes, torch.uint8, "b_codes"), _ptr(b_scales, torch.uint8, "b_scales")
+    po, pw = _ptr(out, out.dtype, "out"), _ptr(ws, torch.uint8, "ws")
+    if K < 1:
+        raise ValueError("K must be at least 1")
+    a_strides, b_strides = _packed(a_codes, a_scales, M, K, "a_"), _packed(b_codes, b_scales, N, K, "b_")
+    with _on_device(a_codes, a_scales, b_codes, b_scales, out, ws):
+        rc = load().gtopk_scaled_product(pa, a_strides[0], pas, a_strides[1], pb, b_strides[0], pbs, b_strides[1], M, N, K,
+                                         po, dtype, stride, pw, ws.numel(), _stream())
+    _check(rc, "gtopk_scaled_product")
+
+
+def gtopk_weight_grad_workspace_bytes(rows: int, P: int, N: int, K: int) -> int:
+    return int(load().gtopk_weight_grad_workspace_bytes(rows, P, N, K))
+
+
+def alloc_weight_grad_workspace(rows: int, P: int, N: int, K: int, device="cuda"):
+    torch = _torch()
+    n = gtopk_weight_grad_workspace_bytes(rows, P, N, K)
+    if n == 0:
+        raise GtopkError(GTOPK_EINVAL, "gtopk_weight_grad_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def gtopk_weight_grad(dy, codes, scales, row_begin, grad, accumulate: bool, ws) -> None:
+    """grad: float32 [P][N][K], for example grads[:, at:at + N*K].unflatten(1, (N, K)) of the workers' gradient rows;
+    row_begin: int32 [P + 1] on the GPU, or None for equal shares."""
+    torch = _torch()
+    dtype = _dtype_code(dy, "dy")
+    rows, N, dy_stride = _dense(dy, "dy")
+    if grad.dim() != 3 or grad.shape[1] != N or grad.shape[0] < 1 or grad.shape[2] < 1:
+        raise ValueError("grad must be [P][N][K], with as many rows as dy has columns")
+    P, _, K = grad.shape
+    if (K > 1 and grad.stride(2) != 1) or (N > 1 and grad.stride(1) != K):
+        raise ValueError("grad must hold each worker's N x K weights contiguously")
+    pd, pc, ps = _ptr(dy, dy.dtype, "dy"), _ptr(codes, torch.uint8, "codes"), _ptr(scales, torch.uint8, "scales")
+    pb = _ptr(row_begin, torch.int32, "row_begin", allow_none=True)
+    if row_begin is not None and (row_begin.dim() != 1 or row_begin.numel() != P + 1 or row_begin.stride(0) != 1):
+        raise ValueError("row_begin must hold P + 1 entries")
+    pg, pw = _ptr(grad, torch.float32, "grad"), _ptr(ws, torch.uint8, "ws")
+    code_stride, scale_stride = _packed(codes, scales, rows, K, "")
+    with _on_device(dy, codes, scales, row_begin, grad, ws):
+        rc = load().gtopk_weight_grad(pd, dtype, dy_stride, pc, code_stride, ps, scale_stride, rows, pb, P, N, K, pg,
+                                      grad.stride(0) if P > 1 else N * K, 1 if accumulate else 0, pw, ws.numel(), _stream())
+    _check(rc, "gtopk_weight_grad")

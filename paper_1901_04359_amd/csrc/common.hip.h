@@ -201,13 +201,4 @@ static_assert(Digit::kLinBins + ((Digit::kTopOctave - Digit::kLinLog2 + 1) << Di
 constexpr int kZeroSlots = 6;
 struct ZeroJob { uint32_t* p[kZeroSlots]; size_t n[kZeroSlots]; };
 
-// clears up to six arrays in one launch (an array with n == 0 is skipped)
-__global__ void k_zero_u32(ZeroJob job) {
-    const size_t step = (size_t)gridDim.x * blockDim.x;
-    const size_t first = (size_t)blockIdx.x * blockDim.x + threadIdx.x;
-#pragma unroll
-    for (int a = 0; a < kZeroSlots; ++a)
-        for (size_t i = first; i < job.n[a]; i += step) job.p[a][i] = 0u;
-}
-
 }  // namespace gtopk

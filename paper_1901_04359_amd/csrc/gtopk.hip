@@ -43,6 +43,15 @@ using namespace gtopk;
 
 namespace {
 
+// clears up to six arrays in one launch (an array with n == 0 is skipped)
+__global__ void k_zero_u32(ZeroJob job) {
+    const size_t step = (size_t)gridDim.x * blockDim.x;
+    const size_t first = (size_t)blockIdx.x * blockDim.x + threadIdx.x;
+#pragma unroll
+    for (int a = 0; a < kZeroSlots; ++a)
+        for (size_t i = first; i < job.n[a]; i += step) job.p[a][i] = 0u;
+}
+
 // ---------------------------------------------------------------------------------
 // host side
 // ---------------------------------------------------------------------------------

@@ -1,0 +1,186 @@
+// What lies before the hot path in an iteration (Algorithm 4 lines 2-3, where the gradients come from): a layer's
+// activations packed to 8 bits, the products that read them, and the weight gradients of P workers written into
+// the gradient rows that gtopk_step takes.  The C ABI's side of packed.hip.h, product.hip.h and weight_grad.hip.h.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "gtopk.h"
+#include "common.hip.h"
+#include "packed.hip.h"
+#include "product.hip.h"
+#include "weight_grad.hip.h"
+
+using namespace gtopk;
+
+namespace {
+
+constexpr int64_t kMaxSide = 0x7FFFFFFF;            // rows and columns of a matrix
+constexpr uint64_t kMaxBlocks = 1u << 22;           // blocks of a launch; kernels walk what is left
+
+inline bool aligned(const void* p, size_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+inline uint32_t grid_for(uint64_t jobs) { return (uint32_t)(jobs < kMaxBlocks ? jobs : kMaxBlocks); }
+inline int launch_status() { return hipGetLastError() == hipSuccess ? GTOPK_OK : GTOPK_EHIP; }
+inline size_t value_bytes(int32_t dtype) { return dtype == GTOPK_F32 ? 4 : 2; }
+inline bool dtype_ok(int32_t dtype) { return dtype == GTOPK_F32 || dtype == GTOPK_BF16 || dtype == GTOPK_F16; }
+inline bool act_ok(int32_t act) { return act >= GTOPK_ACT_NONE && act <= GTOPK_ACT_GELU; }
+inline bool side_ok(int64_t n, int64_t least) { return n >= least && n <= kMaxSide; }
+inline bool packed_strides_ok(int64_t cols, int64_t code_stride, int64_t scale_stride) {
+    const int64_t nb = ceil_div(cols, kPackBlock);
+    return code_stride >= nb * kPackBlock && code_stride % kPackBlock == 0 && scale_stride >= nb && scale_stride % 4 == 0;
+}
+inline bool packed_aligned(const uint8_t* codes, const uint8_t* scales) { return aligned(codes, 16) && aligned(scales, 4); }
+
+// calls launch(F32{}), launch(BF16{}) or launch(F16{})
+template <class L>
+void by_type(int32_t dtype, L launch) {
+    if (dtype == GTOPK_F32) launch(F32{});
+    else if (dtype == GTOPK_BF16) launch(BF16{});
+    else launch(F16{});
+}
+
+PackGrid pack_grid(int64_t rows, int64_t cols, dim3* grid) {
+    PackGrid g;
+    g.rows = rows;
+    g.cols = cols;
+    g.nb = (uint32_t)ceil_div(cols, kPackBlock);
+    g.side_log2 = 0;
+    while (g.side_log2 < 4 && (1u << g.side_log2) < g.nb) ++g.side_log2;
+    const int64_t deep = (kPackThreads / 16) >> g.side_log2, down = ceil_div(rows, deep);
+    *grid = dim3((uint32_t)ceil_div(g.nb, 1 << g.side_log2), (uint32_t)(down < 65535 ? down : 65535));
+    return g;
+}
+
+}  // namespace
+
+extern "C" {
+
+int gtopk_pack_rows(const void* x, int32_t dtype, int64_t rows, int64_t cols, int64_t stride, uint8_t* codes,
+                    int64_t code_stride, uint8_t* scales, int64_t scale_stride, void* stream) {
+    if (!dtype_ok(dtype) || !side_ok(rows, 0) || !side_ok(cols, 1) || stride < cols) return GTOPK_EINVAL;
+    if (!packed_strides_ok(cols, code_stride, scale_stride)) return GTOPK_EINVAL;
+    if (rows == 0) return GTOPK_OK;
+    if (!x || !codes || !scales) return GTOPK_EINVAL;
+    if (!aligned(x, value_bytes(dtype)) || !packed_aligned(codes, scales)) return GTOPK_EALIGN;
+    dim3 grid;
+    const PackGrid g = pack_grid(rows, cols, &grid);
+    by_type(dtype, [&](auto d) {
+        using D = decltype(d);
+        hipLaunchKernelGGL(k_pack_rows<D>, grid, dim3(kPackThreads), 0, (hipStream_t)stream, (const typename D::T*)x, stride, g,
+                           codes, code_stride, scales, scale_stride);
+    });
+    return launch_status();
+}
+
+int gtopk_pack_tiles(const void* x, int32_t dtype, int64_t rows, int64_t cols, int64_t stride, uint8_t* codes,
+                     int64_t code_stride, uint8_t* scales, int64_t scale_stride, uint8_t* codes_t, int64_t code_t_stride,
+                     uint8_t* scales_t, int64_t scale_t_stride, void* stream) {
+    if (!dtype_ok(dtype) || !side_ok(rows, 0) || !side_ok(cols, 1) || stride < cols) return GTOPK_EINVAL;
+    if (rows == 0) return GTOPK_OK;
+    if (!x || (!codes && !codes_t) || (codes == nullptr) != (scales == nullptr) || (codes_t == nullptr) != (scales_t == nullptr))
+        return GTOPK_EINVAL;
+    if ((codes && !packed_strides_ok(cols, code_stride, scale_stride)) || (codes_t && !packed_strides_ok(rows, code_t_stride, scale_t_stride)))
+        return GTOPK_EINVAL;
+    if (!aligned(x, value_bytes(dtype)) || !packed_aligned(codes, scales) || !packed_aligned(codes_t, scales_t)) return GTOPK_EALIGN;
+    const uint32_t nbc = (uint32_t)ceil_div(cols, kPackBlock);
+    const uint64_t tiles = (uint64_t)ceil_div(rows, kPackBlock) * nbc;
+    by_type(dtype, [&](auto d) {
+        using D = decltype(d);
+        hipLaunchKernelGGL(k_pack_tiles<D>, dim3(grid_for(tiles)), dim3(kPackThreads), 0, (hipStream_t)stream,
+                           (const typename D::T*)x, stride, rows, cols, codes, code_stride, scales, scale_stride, codes_t,
+                           code_t_stride, scales_t, scale_t_stride, nbc, tiles);
+    });
+    return launch_status();
+}
+
+int gtopk_unpack(const uint8_t* codes, int64_t code_stride, const uint8_t* scales, int64_t scale_stride, int64_t rows,
+                 int64_t cols, int32_t act, void* out, int32_t dtype, int64_t out_stride, void* stream) {
+    if (!dtype_ok(dtype) || !act_ok(act) || !side_ok(rows, 0) || !side_ok(cols, 1) || out_stride < cols) return GTOPK_EINVAL;
+    if (!packed_strides_ok(cols, code_stride, scale_stride)) return GTOPK_EINVAL;
+    if (rows == 0) return GTOPK_OK;
+    if (!codes || !scales || !out) return GTOPK_EINVAL;
+    if (!packed_aligned(codes, scales) || !aligned(out, value_bytes(dtype))) return GTOPK_EALIGN;
+    dim3 grid;
+    const PackGrid g = pack_grid(rows, cols, &grid);
+    by_type(dtype, [&](auto d) {
+        using D = decltype(d);
+        hipLaunchKernelGGL(k_unpack<D>, grid, dim3(kPackThreads), 0, (hipStream_t)stream, codes, code_stride, scales,
+                           scale_stride, g, (int)act, (typename D::T*)out, out_stride);
+    });
+    return launch_status();
+}
+
+int gtopk_activation_grad(const uint8_t* codes, int64_t code_stride, const uint8_t* scales, int64_t scale_stride,
+                          int64_t rows, int64_t cols, int32_t act, const void* dy, int64_t dy_stride, void* dx,
+                          int64_t dx_stride, int32_t dtype, void* stream) {
+    if (!dtype_ok(dtype) || !act_ok(act) || !side_ok(rows, 0) || !side_ok(cols, 1) || dy_stride < cols || dx_stride < cols)
+        return GTOPK_EINVAL;
+    if (!packed_strides_ok(cols, code_stride, scale_stride)) return GTOPK_EINVAL;
+    if (rows == 0) return GTOPK_OK;
+    if (!codes || !scales || !dy || !dx || (dy == dx && dy_stride != dx_stride)) return GTOPK_EINVAL;
+    if (!packed_aligned(codes, scales) || !aligned(dy, value_bytes(dtype)) || !aligned(dx, value_bytes(dtype))) return GTOPK_EALIGN;
+    dim3 grid;
+    const PackGrid g = pack_grid(rows, cols, &grid);
+    by_type(dtype, [&](auto d) {
+        using D = decltype(d);
+        hipLaunchKernelGGL(k_activation_grad<D>, grid, dim3(kPackThreads), 0, (hipStream_t)stream, codes, code_stride, scales,
+                           scale_stride, g, (int)act, (const typename D::T*)dy, dy_stride, (typename D::T*)dx, dx_stride);
+    });
+    return launch_status();
+}
+
+size_t gtopk_product_workspace_bytes(int64_t M, int64_t N, int64_t K) {
+    if (!side_ok(M, 0) || !side_ok(N, 1) || !side_ok(K, 1)) return 0;
+    return 256;
+}
+
+int gtopk_scaled_product(const uint8_t* a_codes, int64_t a_code_stride, const uint8_t* a_scales, int64_t a_scale_stride,
+                         const uint8_t* b_codes, int64_t b_code_stride, const uint8_t* b_scales, int64_t b_scale_stride,
+                         int64_t M, int64_t N, int64_t K, void* out, int32_t dtype, int64_t out_stride, void* ws,
+                         size_t ws_bytes, void* stream) {
+    const size_t need = gtopk_product_workspace_bytes(M, N, K);
+    if (!need || !dtype_ok(dtype) || out_stride < N) return GTOPK_EINVAL;
+    if (!packed_strides_ok(K, a_code_stride, a_scale_stride) || !packed_strides_ok(K, b_code_stride, b_scale_stride)) return GTOPK_EINVAL;
+    if (M == 0) return GTOPK_OK;
+    if (!a_codes || !a_scales || !b_codes || !b_scales || !out || !ws) return GTOPK_EINVAL;
+    if (!packed_aligned(a_codes, a_scales) || !packed_aligned(b_codes, b_scales) || !aligned(out, value_bytes(dtype)) || !aligned(ws, 16))
+        return GTOPK_EALIGN;
+    if (ws_bytes < need) return GTOPK_EWORKSPACE;
+    const uint32_t tiles_n = (uint32_t)ceil_div(N, 16);
+    const uint64_t tiles = (uint64_t)ceil_div(M, 16) * tiles_n;
+    by_type(dtype, [&](auto d) {
+        using D = decltype(d);
+        hipLaunchKernelGGL(k_product<D>, dim3(grid_for(tiles)), dim3(256), 0, (hipStream_t)stream, a_codes, a_code_stride, a_scales,
+                           a_scale_stride, b_codes, b_code_stride, b_scales, b_scale_stride, M, N, (uint32_t)ceil_div(K, kPackBlock),
+                           (typename D::T*)out, out_stride, tiles_n, tiles);
+    });
+    return launch_status();
+}
+
+size_t gtopk_weight_grad_workspace_bytes(int64_t rows, int32_t P, int64_t N, int64_t K) {
+    if (!side_ok(rows, 0) || P < 1 || P > 32768 || !side_ok(N, 1) || !side_ok(K, 1)) return 0;
+    return 256;
+}
+
+int gtopk_weight_grad(const void* dy, int32_t dtype, int64_t dy_stride, const uint8_t* codes, int64_t code_stride,
+                      const uint8_t* scales, int64_t scale_stride, int64_t rows, const int32_t* row_begin, int32_t P, int64_t N,
+                      int64_t K, float* grad, int64_t grad_stride, int32_t accumulate, void* ws, size_t ws_bytes, void* stream) {
+    const size_t need = gtopk_weight_grad_workspace_bytes(rows, P, N, K);
+    if (!need || !dtype_ok(dtype) || dy_stride < N || !packed_strides_ok(K, code_stride, scale_stride)) return GTOPK_EINVAL;
+    if ((P > 1 && grad_stride < N * K) || (!row_begin && rows % P != 0)) return GTOPK_EINVAL;
+    if ((rows > 0 && (!dy || !codes || !scales)) || !grad || !ws) return GTOPK_EINVAL;
+    if (!aligned(dy, value_bytes(dtype)) || !packed_aligned(codes, scales) || !aligned(row_begin, 4) || !aligned(grad, 4) || !aligned(ws, 16))
+        return GTOPK_EALIGN;
+    if (ws_bytes < need) return GTOPK_EWORKSPACE;
+    const uint32_t tiles_k = (uint32_t)ceil_div(K, 16);
+    const uint64_t tiles = (uint64_t)ceil_div(N, 16) * tiles_k;
+    by_type(dtype, [&](auto d) {
+        using D = decltype(d);
+        hipLaunchKernelGGL(k_weight_grad<D>, dim3(grid_for(tiles * (uint64_t)P)), dim3(256), 0, (hipStream_t)stream,
+                           (const typename D::T*)dy, dy_stride, codes, code_stride, scales, scale_stride, rows, row_begin, (uint32_t)P,
+                           N, K, grad, grad_stride, accumulate ? 1 : 0, tiles_k, tiles);
+    });
+    return launch_status();
+}
+
+}  // extern "C"

@@ -1,0 +1,293 @@
+// Packed matrices: values in 8-bit floating point (e4m3: sign, 4 exponent bits, 3 mantissa bits) with one
+// power-of-two scale per block of 128 values of a row, and what reads and writes them value by value.
+//
+// With e the smallest integer for which a block's largest magnitude is at most 448 * 2^e (448 = 1.75 * 2^8 is
+// the largest e4m3 number), a value x is stored as the e4m3 number nearest to x * 2^-e.  The scale is a power of
+// two, so x * 2^-e and code * 2^e are exact and the one rounding is the code's own: at most 2^-4 of the value
+// above 2^-6 * 2^e, at most 2^-10 * 2^e below.  A scale of 32 bits would bring every block's largest value to exactly 448,
+// which buys a floating-point code less than one binade of its 15 at the small end and nothing else, and
+// would cost a multiply per product and block; a power of two goes into the matrix instruction as its scale operand.
+//
+// Every kernel here moves each byte once and is bound by HBM bandwidth.
+#pragma once
+#include "common.hip.h"
+
+namespace gtopk {
+
+constexpr int kPackBlock = 128;             // values per scale
+constexpr int kLaneVals = 8;                // consecutive values a lane handles: 16 lanes cover one block
+constexpr int kPackThreads = 256;           // 16 blocks of 128 side by side
+
+typedef uint32_t uint32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t uint32x4 __attribute__((ext_vector_type(4)));
+typedef float floatx2 __attribute__((ext_vector_type(2)));
+
+// dense matrices hold one of three types; they need only that type's own alignment, and rows at any stride
+struct F32 { typedef float T; };
+struct BF16 { typedef __bf16 T; };
+struct F16 { typedef _Float16 T; };
+
+// 8 consecutive values; p is aligned to one value (global memory takes wide accesses at any address)
+template <class D>
+__device__ __forceinline__ void load8(const typename D::T* p, float (&v)[kLaneVals]) {
+    typedef typename D::T T;
+    typedef T Vec __attribute__((ext_vector_type(kLaneVals)));
+    struct __attribute__((packed)) Loose { Vec v; };
+    const Vec x = reinterpret_cast<const Loose*>(p)->v;
+#pragma unroll
+    for (int j = 0; j < kLaneVals; ++j) v[j] = (float)x[j];
+}
+template <class D>
+__device__ __forceinline__ void store8(typename D::T* p, const float (&v)[kLaneVals]) {
+    typedef typename D::T T;
+    typedef T Vec __attribute__((ext_vector_type(kLaneVals)));
+    struct __attribute__((packed)) Loose { Vec v; };
+    Vec x;
+#pragma unroll
+    for (int j = 0; j < kLaneVals; ++j) x[j] = (T)v[j];      // to nearest, ties to even
+    reinterpret_cast<Loose*>(p)->v = x;
+}
+// the same of the n < 8 values that a row's end leaves; 0 behind them
+template <class D>
+__device__ __forceinline__ void load_some(const typename D::T* p, int n, float (&v)[kLaneVals]) {
+#pragma unroll
+    for (int j = 0; j < kLaneVals; ++j) v[j] = j < n ? (float)p[j] : 0.0f;
+}
+template <class D>
+__device__ __forceinline__ void store_some(typename D::T* p, int n, const float (&v)[kLaneVals]) {
+#pragma unroll
+    for (int j = 0; j < kLaneVals; ++j)
+        if (j < n) p[j] = (typename D::T)v[j];
+}
+
+// 2^(s - 127); 255 stands for NaN
+__device__ __forceinline__ float scale_value(uint32_t s) {
+    return __uint_as_float(s == 0u ? 0x00400000u : s == 255u ? 0x7FC00000u : s << 23);
+}
+// the stored exponent e + 127 for a block whose largest finite magnitude has these bits
+__device__ __forceinline__ uint32_t scale_for(uint32_t top) {
+    const int s = (int)(top >> 23) - 8 + ((top & 0x7FFFFFu) > 0x600000u ? 1 : 0);
+    return s < 0 ? 0u : (uint32_t)s;
+}
+// 2^-e of a stored exponent that scale_for returned (0 .. 247)
+__device__ __forceinline__ float inverse_scale(uint32_t s) { return __uint_as_float((254u - s) << 23); }
+
+__device__ __forceinline__ bool finite_bits(uint32_t b) { return (b & 0x7F800000u) != 0x7F800000u; }
+
+// bits of the largest finite magnitude among 8 values
+__device__ __forceinline__ uint32_t top_of(const float (&v)[kLaneVals]) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int j = 0; j < kLaneVals; ++j) {
+        const uint32_t b = __float_as_uint(v[j]) & kAbs;
+        if (finite_bits(b) && b > top) top = b;
+    }
+    return top;
+}
+// maximum over the 16 lanes of a DPP row, in all of them (row_ror:n = 0x120 + n)
+__device__ __forceinline__ uint32_t row_largest(uint32_t v) {
+    auto with = [&](uint32_t x) { v = x > v ? x : v; };
+    with(dpp_moved<0x128, 0xf>(v));
+    with(dpp_moved<0x124, 0xf>(v));
+    with(dpp_moved<0x122, 0xf>(v));
+    with(dpp_moved<0x121, 0xf>(v));
+    return v;
+}
+// the codes of 8 values; what is not finite becomes the NaN code (e4m3 has no infinity), so that an overflow
+// in the forward pass reaches the gradients instead of passing for a large value
+__device__ __forceinline__ uint32x2 encode8(const float (&v)[kLaneVals], float inv) {
+    float y[kLaneVals];
+#pragma unroll
+    for (int j = 0; j < kLaneVals; ++j)
+        y[j] = finite_bits(__float_as_uint(v[j])) ? v[j] * inv : __uint_as_float(0x7FC00000u);
+    uint32x2 c;
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+    c[0] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], w, true);
+    w = __builtin_amdgcn_cvt_pk_fp8_f32(y[4], y[5], 0, false);
+    c[1] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[6], y[7], w, true);
+    return c;
+}
+__device__ __forceinline__ void decode8(uint32x2 c, float scale, float (&v)[kLaneVals]) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const floatx2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)c[h], false);
+        const floatx2 hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)c[h], true);
+        v[4 * h] = lo[0] * scale;
+        v[4 * h + 1] = lo[1] * scale;
+        v[4 * h + 2] = hi[0] * scale;
+        v[4 * h + 3] = hi[1] * scale;
+    }
+}
+
+// How the 16 blocks of 128 that a thread block covers lie in the matrix: 2^side_log2 of them side by side, the rest below
+struct PackGrid {
+    int64_t rows, cols;
+    uint32_t nb;                            // blocks of 128 per row
+    uint32_t side_log2;
+};
+// f(row, block of the row, lane's first column) for every block of 128, 16 lanes per block, all lanes of a row together
+template <class F>
+__device__ __forceinline__ void for_blocks(const PackGrid& g, F f) {
+    const uint32_t item = threadIdx.x / 16, lane = threadIdx.x % 16;
+    const uint32_t kb = (blockIdx.x << g.side_log2) + (item & ((1u << g.side_log2) - 1u));
+    const uint32_t deep = (kPackThreads / 16) >> g.side_log2;      // rows per thread block
+    if (kb >= g.nb) return;
+    for (int64_t row = (int64_t)blockIdx.y * deep + (item >> g.side_log2); row < g.rows; row += (int64_t)gridDim.y * deep)
+        f(row, kb, (int64_t)kb * kPackBlock + lane * kLaneVals);
+}
+
+template <class D>
+__global__ __launch_bounds__(kPackThreads) void k_pack_rows(
+        const typename D::T* __restrict__ x, int64_t stride, PackGrid g, uint8_t* __restrict__ codes, int64_t code_stride,
+        uint8_t* __restrict__ scales, int64_t scale_stride) {
+    for_blocks(g, [&](int64_t row, uint32_t kb, int64_t col) {
+        float v[kLaneVals];
+        const int64_t left = g.cols - col;
+        const typename D::T* p = x + row * stride + col;
+        if (left >= kLaneVals) load8<D>(p, v);
+        else load_some<D>(p, (int)left, v);
+        const uint32_t s = scale_for(row_largest(top_of(v)));
+        *reinterpret_cast<uint32x2*>(codes + row * code_stride + col) = encode8(v, inverse_scale(s));
+        if (threadIdx.x % 16 == 0) scales[row * scale_stride + kb] = (uint8_t)s;
+    });
+}
+
+// f and f' of the layer's activation, in 32 bits
+__device__ __forceinline__ float logistic(float x) { return 1.0f / (1.0f + expf(-x)); }
+__device__ __forceinline__ float act_value(int act, float x) {
+    switch (act) {
+        case GTOPK_ACT_RELU: return x < 0.0f ? 0.0f : x;              // NaN stays NaN
+        case GTOPK_ACT_TANH: return tanhf(x);
+        case GTOPK_ACT_SIGMOID: return logistic(x);
+        case GTOPK_ACT_SILU: return x * logistic(x);
+        case GTOPK_ACT_GELU: return x * 0.5f * erfcf(x * -0.70710678118654752f);
+        default: return x;
+    }
+}
+__device__ __forceinline__ float act_slope(int act, float x) {
+    switch (act) {
+        case GTOPK_ACT_RELU: return x > 0.0f ? 1.0f : x <= 0.0f ? 0.0f : x;
+        case GTOPK_ACT_TANH: { const float t = tanhf(x); return (1.0f - t) * (1.0f + t); }
+        case GTOPK_ACT_SIGMOID: return logistic(x) * logistic(-x);
+        case GTOPK_ACT_SILU: { const float s = logistic(x); return s + x * (s * logistic(-x)); }
+        case GTOPK_ACT_GELU:
+            return 0.5f * erfcf(x * -0.70710678118654752f) + x * (0.39894228040143268f * expf(-0.5f * x * x));
+        default: return x == x ? 1.0f : x;
+    }
+}
+
+template <class D>
+__global__ __launch_bounds__(kPackThreads) void k_unpack(
+        const uint8_t* __restrict__ codes, int64_t code_stride, const uint8_t* __restrict__ scales, int64_t scale_stride,
+        PackGrid g, int act, typename D::T* __restrict__ out, int64_t stride) {
+    for_blocks(g, [&](int64_t row, uint32_t kb, int64_t col) {
+        float v[kLaneVals];
+        decode8(*reinterpret_cast<const uint32x2*>(codes + row * code_stride + col),
+                scale_value(scales[row * scale_stride + kb]), v);
+#pragma unroll
+        for (int j = 0; j < kLaneVals; ++j) v[j] = act_value(act, v[j]);
+        const int64_t left = g.cols - col;
+        typename D::T* p = out + row * stride + col;
+        if (left >= kLaneVals) store8<D>(p, v);
+        else store_some<D>(p, (int)left, v);
+    });
+}
+
+// dx may be dy: a lane reads its values before it writes them, and nobody else touches them
+template <class D>
+__global__ __launch_bounds__(kPackThreads) void k_activation_grad(
+        const uint8_t* __restrict__ codes, int64_t code_stride, const uint8_t* __restrict__ scales, int64_t scale_stride,
+        PackGrid g, int act, const typename D::T* dy, int64_t dy_stride, typename D::T* dx, int64_t dx_stride) {
+    for_blocks(g, [&](int64_t row, uint32_t kb, int64_t col) {
+        float v[kLaneVals], d[kLaneVals];
+        const int64_t left = g.cols - col;
+        const typename D::T* p = dy + row * dy_stride + col;
+        if (left >= kLaneVals) load8<D>(p, d);
+        else load_some<D>(p, (int)left, d);
+        decode8(*reinterpret_cast<const uint32x2*>(codes + row * code_stride + col),
+                scale_value(scales[row * scale_stride + kb]), v);
+#pragma unroll
+        for (int j = 0; j < kLaneVals; ++j) d[j] *= act_slope(act, v[j]);
+        typename D::T* q = dx + row * dx_stride + col;
+        if (left >= kLaneVals) store8<D>(q, d);
+        else store_some<D>(q, (int)left, d);
+    });
+}
+
+// One thread block per tile of 128 x 128.  Of the tile a thread holds rows 64 h + 16 wave + 4 (lane / 16) + (0 .. 3),
+// h = 0, 1, and 8 columns: four rows, so that the transposed codes come out as whole words.
+constexpr int kTilePitch = kPackBlock / 4 + 1;      // words per row of the transposed tile in LDS: one extra spreads the banks
+template <class D>
+__global__ __launch_bounds__(kPackThreads) void k_pack_tiles(
+        const typename D::T* __restrict__ x, int64_t stride, int64_t rows, int64_t cols, uint8_t* __restrict__ codes,
+        int64_t code_stride, uint8_t* __restrict__ scales, int64_t scale_stride, uint8_t* __restrict__ codes_t,
+        int64_t code_t_stride, uint8_t* __restrict__ scales_t, int64_t scale_t_stride, uint32_t nbc, uint64_t tiles) {
+    __shared__ uint32_t s_t[kPackBlock * kTilePitch];
+    __shared__ uint32_t s_top[kPackThreads / kWave];
+    const uint32_t wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+    for (uint64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+        const int64_t tr = (int64_t)(tile / nbc), tc = (int64_t)(tile % nbc);
+        const int64_t col = tc * kPackBlock + (lane % 16) * kLaneVals;
+        const int64_t left = cols - col;
+        float v[8][kLaneVals];
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int64_t row = tr * kPackBlock + (i / 4) * 64 + wave * 16 + (lane / 16) * 4 + i % 4;
+            const typename D::T* p = x + row * stride + col;
+            if (row < rows && left >= kLaneVals) load8<D>(p, v[i]);
+            else load_some<D>(p, row < rows ? (int)left : 0, v[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t t = top_of(v[i]);
+            top = t > top ? t : top;
+        }
+        top = wave_largest(top);
+        if (lane == 0) s_top[wave] = top;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kPackThreads / kWave; ++i) top = s_top[i] > top ? s_top[i] : top;
+        const uint32_t s = scale_for(top);
+        const float inv = inverse_scale(s);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int64_t row0 = tr * kPackBlock + h * 64 + wave * 16 + (lane / 16) * 4;
+            uint32x2 c[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                c[i] = encode8(v[h * 4 + i], inv);
+                if (codes && row0 + i < rows) *reinterpret_cast<uint32x2*>(codes + (row0 + i) * code_stride + col) = c[i];
+            }
+            if (codes_t) {
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {      // 4 x 4 bytes turned: word j holds column j of the four rows
+                    const uint32_t ab02 = __builtin_amdgcn_perm(c[1][q], c[0][q], 0x06020400u), ab13 = __builtin_amdgcn_perm(c[1][q], c[0][q], 0x07030501u);
+                    const uint32_t cd02 = __builtin_amdgcn_perm(c[3][q], c[2][q], 0x06020400u), cd13 = __builtin_amdgcn_perm(c[3][q], c[2][q], 0x07030501u);
+                    uint32_t* t = s_t + ((lane % 16) * kLaneVals + q * 4) * kTilePitch + (h * 64 + wave * 16 + (lane / 16) * 4) / 4;
+                    t[0] = __builtin_amdgcn_perm(cd02, ab02, 0x05040100u);
+                    t[kTilePitch] = __builtin_amdgcn_perm(cd13, ab13, 0x05040100u);
+                    t[2 * kTilePitch] = __builtin_amdgcn_perm(cd02, ab02, 0x07060302u);
+                    t[3 * kTilePitch] = __builtin_amdgcn_perm(cd13, ab13, 0x07060302u);
+                }
+            }
+        }
+        // the scale of the tile, once for each of its rows, so that readers need not know about tiles
+        if (codes && threadIdx.x < kPackBlock && tr * kPackBlock + threadIdx.x < rows)
+            scales[(tr * kPackBlock + threadIdx.x) * scale_stride + tc] = (uint8_t)s;
+        if (codes_t && threadIdx.x >= kPackBlock && tc * kPackBlock + (threadIdx.x - kPackBlock) < cols)
+            scales_t[(tc * kPackBlock + (threadIdx.x - kPackBlock)) * scale_t_stride + tr] = (uint8_t)s;
+        __syncthreads();
+        if (codes_t) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int r = i * 8 + threadIdx.x / 32, w = threadIdx.x % 32;
+                const int64_t row = tc * kPackBlock + r;
+                if (row < cols) *reinterpret_cast<uint32_t*>(codes_t + row * code_t_stride + tr * kPackBlock + w * 4) = s_t[r * kTilePitch + w];
+            }
+        }
+        __syncthreads();                   // the next tile writes s_top and s_t
+    }
+}
+
+}  // namespace gtopk
