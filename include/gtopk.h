@@ -310,9 +310,13 @@ int gtopk_activation_grad(const uint8_t* codes, int64_t code_stride, const uint8
                           void* dx, int64_t dx_stride, int32_t dtype, void* stream);
 
 /*
- * out = A B^T for packed A (M x K) and packed B (N x K): out[m][n] = sum over k of A[m][k] * B[n][k].  Products are
- * exact, sums are fp32, the result is rounded once to dtype.  Forward pass of a layer: A its packed input, B its
- * packed weights; input gradient: A the packed output gradient, B the transposed packed weights.
+ * out = A B^T for packed A (M x K) and packed B (N x K): out[m][n] = sum over k of A[m][k] * B[n][k], rounded once to
+ * dtype.  Forward pass of a layer: A its packed input, B its packed weights; input gradient: A the packed output
+ * gradient, B the transposed packed weights.
+ *   GTOPK_F32:  products are exact, sums are fp32 (magnitudes below 2^-126 may be rounded to a multiple of 2^-133).
+ *   GTOPK_BF16, GTOPK_F16: twice as fast.  The eight products of k = 8 j .. 8 j + 7 are exact, but each is cut
+ *               off at 2^-13 of the largest of the eight (its leading bit); all further sums are fp32.
+ *   Code strides (and so K) of at most 2^23.
  *   ws : gtopk_product_workspace_bytes(M, N, K) bytes (0 if the sizes are invalid)
  */
 size_t gtopk_product_workspace_bytes(int64_t M, int64_t N, int64_t K);

@@ -15,6 +15,7 @@ using namespace gtopk;
 namespace {
 
 constexpr int64_t kMaxSide = 0x7FFFFFFF;            // rows and columns of a matrix
+constexpr int64_t kMaxCodeStride = 1 << 23;         // of a product's operands: a tile's rows at offsets of 32 bits
 constexpr uint64_t kMaxBlocks = 1u << 22;           // blocks of a launch; kernels walk what is left
 
 inline bool aligned(const void* p, size_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
@@ -48,6 +49,29 @@ PackGrid pack_grid(int64_t rows, int64_t cols, dim3* grid) {
     while (g.side_log2 < 4 && (1u << g.side_log2) < g.nb) ++g.side_log2;
     const int64_t deep = (kPackThreads / 16) >> g.side_log2, down = ceil_div(rows, deep);
     *grid = dim3((uint32_t)ceil_div(g.nb, 1 << g.side_log2), (uint32_t)(down < 65535 ? down : 65535));
+    return g;
+}
+
+// How the weight gradient's sums are cut: tiles of 128 x 128 of every worker, and where they are too few for the
+// chip's 256 compute units (two blocks each), shares of the rows, at least kGradShareRows long, summed from the workspace.
+struct GradPlan {
+    uint32_t tiles_n, tiles_k, splits;
+    int64_t part_stride;                // values of one worker's share
+    uint64_t jobs;
+};
+constexpr uint64_t kGradBlocks = 512;
+constexpr int64_t kGradShareRows = 256;
+constexpr uint64_t kMaxJobs = 0x7FFFFFFF;
+GradPlan grad_plan(int64_t rows, int32_t P, int64_t N, int64_t K) {
+    GradPlan g;
+    g.tiles_n = (uint32_t)ceil_div(N, 128);
+    g.tiles_k = (uint32_t)ceil_div(K, 128);
+    const uint64_t blocks = (uint64_t)g.tiles_n * g.tiles_k * (uint64_t)P;
+    const int64_t most = rows / P / kGradShareRows, want = (int64_t)(kGradBlocks / blocks);
+    g.splits = (uint32_t)(want < most ? want : most);
+    if (g.splits < 1) g.splits = 1;
+    g.part_stride = ceil_div(N * K, 4) * 4;
+    g.jobs = blocks * g.splits;
     return g;
 }
 
@@ -130,7 +154,7 @@ int gtopk_activation_grad(const uint8_t* codes, int64_t code_stride, const uint8
 }
 
 size_t gtopk_product_workspace_bytes(int64_t M, int64_t N, int64_t K) {
-    if (!side_ok(M, 0) || !side_ok(N, 1) || !side_ok(K, 1)) return 0;
+    if (!side_ok(M, 0) || !side_ok(N, 1) || !side_ok(K, 1) || K > kMaxCodeStride) return 0;
     return 256;
 }
 
@@ -141,25 +165,32 @@ int gtopk_scaled_product(const uint8_t* a_codes, int64_t a_code_stride, const ui
     const size_t need = gtopk_product_workspace_bytes(M, N, K);
     if (!need || !dtype_ok(dtype) || out_stride < N) return GTOPK_EINVAL;
     if (!packed_strides_ok(K, a_code_stride, a_scale_stride) || !packed_strides_ok(K, b_code_stride, b_scale_stride)) return GTOPK_EINVAL;
+    if (a_code_stride > kMaxCodeStride || b_code_stride > kMaxCodeStride) return GTOPK_EINVAL;
     if (M == 0) return GTOPK_OK;
     if (!a_codes || !a_scales || !b_codes || !b_scales || !out || !ws) return GTOPK_EINVAL;
     if (!packed_aligned(a_codes, a_scales) || !packed_aligned(b_codes, b_scales) || !aligned(out, value_bytes(dtype)) || !aligned(ws, 16))
         return GTOPK_EALIGN;
     if (ws_bytes < need) return GTOPK_EWORKSPACE;
-    const uint32_t tiles_n = (uint32_t)ceil_div(N, 16);
-    const uint64_t tiles = (uint64_t)ceil_div(M, 16) * tiles_n;
+    const PackedMatrix a{a_codes, a_scales, (uint32_t)a_code_stride, (uint32_t)a_scale_stride};
+    const PackedMatrix b{b_codes, b_scales, (uint32_t)b_code_stride, (uint32_t)b_scale_stride};
     by_type(dtype, [&](auto d) {
         using D = decltype(d);
-        hipLaunchKernelGGL(k_product<D>, dim3(grid_for(tiles)), dim3(256), 0, (hipStream_t)stream, a_codes, a_code_stride, a_scales,
-                           a_scale_stride, b_codes, b_code_stride, b_scales, b_scale_stride, M, N, (uint32_t)ceil_div(K, kPackBlock),
-                           (typename D::T*)out, out_stride, tiles_n, tiles);
+#ifndef CFG
+#define CFG 128, 128, 64, 64
+#endif
+        constexpr int c[4] = {CFG};
+        const uint32_t tiles_m = (uint32_t)ceil_div(M, c[0]), tiles_n = (uint32_t)ceil_div(N, c[1]);
+        hipLaunchKernelGGL((k_product<D, CFG>), dim3(tiles_m * tiles_n), dim3((c[0] / c[2]) * (c[1] / c[3]) * kWave), 0,
+                           (hipStream_t)stream, a, b, M, N, (uint32_t)ceil_div(K, kPackBlock), (typename D::T*)out, out_stride, tiles_m, tiles_n);
     });
     return launch_status();
 }
 
 size_t gtopk_weight_grad_workspace_bytes(int64_t rows, int32_t P, int64_t N, int64_t K) {
     if (!side_ok(rows, 0) || P < 1 || P > 32768 || !side_ok(N, 1) || !side_ok(K, 1)) return 0;
-    return 256;
+    const GradPlan g = grad_plan(rows, P, N, K);
+    if (g.jobs > kMaxJobs) return 0;
+    return 256 + (g.splits > 1 ? (size_t)g.splits * P * g.part_stride * sizeof(float) : 0);
 }
 
 int gtopk_weight_grad(const void* dy, int32_t dtype, int64_t dy_stride, const uint8_t* codes, int64_t code_stride,
@@ -172,14 +203,21 @@ int gtopk_weight_grad(const void* dy, int32_t dtype, int64_t dy_stride, const ui
     if (!aligned(dy, value_bytes(dtype)) || !packed_aligned(codes, scales) || !aligned(row_begin, 4) || !aligned(grad, 4) || !aligned(ws, 16))
         return GTOPK_EALIGN;
     if (ws_bytes < need) return GTOPK_EWORKSPACE;
-    const uint32_t tiles_k = (uint32_t)ceil_div(K, 16);
-    const uint64_t tiles = (uint64_t)ceil_div(N, 16) * tiles_k;
+    const GradPlan g = grad_plan(rows, P, N, K);
+    const bool split = g.splits > 1;
+    hipStream_t st = (hipStream_t)stream;
     by_type(dtype, [&](auto d) {
         using D = decltype(d);
-        hipLaunchKernelGGL(k_weight_grad<D>, dim3(grid_for(tiles * (uint64_t)P)), dim3(256), 0, (hipStream_t)stream,
-                           (const typename D::T*)dy, dy_stride, codes, code_stride, scales, scale_stride, rows, row_begin, (uint32_t)P,
-                           N, K, grad, grad_stride, accumulate ? 1 : 0, tiles_k, tiles);
+        hipLaunchKernelGGL((k_weight_grad<D, 128, 128, 64, 64>), dim3(grid_for(g.jobs)), dim3(256), 0, st, (const typename D::T*)dy,
+                           dy_stride, codes, code_stride, scales, scale_stride, rows, row_begin, (uint32_t)P, N, K,
+                           split ? (float*)ws : grad, split ? g.part_stride : grad_stride, split ? 0 : accumulate != 0, g.splits,
+                           split ? g.part_stride * P : 0, g.tiles_n, g.tiles_k, (uint32_t)g.jobs);
     });
+    if (split) {
+        const int64_t blocks = ceil_div(N * K, 4 * kPackThreads);
+        hipLaunchKernelGGL(k_join_shares, dim3((uint32_t)(blocks < 4096 ? blocks : 4096), (uint32_t)P), dim3(kPackThreads), 0, st,
+                           (const float*)ws, g.splits, g.part_stride * P, g.part_stride, N * K, grad, grad_stride, accumulate != 0);
+    }
     return launch_status();
 }
 

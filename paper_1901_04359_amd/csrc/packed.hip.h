@@ -60,6 +60,24 @@ __device__ __forceinline__ void store_some(typename D::T* p, int n, const float 
         if (j < n) p[j] = (typename D::T)v[j];
 }
 
+// 4 consecutive values, of which a row's end leaves `left`
+template <class D>
+__device__ __forceinline__ void store4(typename D::T* p, int64_t left, floatx4 v) {
+    typedef typename D::T T;
+    typedef T Vec __attribute__((ext_vector_type(4)));
+    struct __attribute__((packed)) Loose { Vec v; };
+    if (left >= 4) {
+        Vec x;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = (T)v[j];
+        reinterpret_cast<Loose*>(p)->v = x;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (j < left) p[j] = (T)v[j];
+    }
+}
+
 // 2^(s - 127); 255 stands for NaN
 __device__ __forceinline__ float scale_value(uint32_t s) {
     return __uint_as_float(s == 0u ? 0x00400000u : s == 255u ? 0x7FC00000u : s << 23);
@@ -117,6 +135,17 @@ __device__ __forceinline__ void decode8(uint32x2 c, float scale, float (&v)[kLan
         v[4 * h + 2] = hi[0] * scale;
         v[4 * h + 3] = hi[1] * scale;
     }
+}
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+// the lower (upper) two codes of a word as bf16 numbers times a power of two: exact down to 2^-126, below that
+// rounded to a multiple of 2^-133.  (The word is taken whole: taking the vector's elements apart gives the first one twice.)
+template <bool UPPER>
+__device__ __forceinline__ uint32_t decode2(uint32_t c, float scale) {
+    const bf16x2 v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, scale, UPPER);
+    return __builtin_bit_cast(uint32_t, v);
 }
 
 // How the 16 blocks of 128 that a thread block covers lie in the matrix: 2^side_log2 of them side by side, the rest below

@@ -1,38 +1,182 @@
 // C = A B^T of two packed matrices:
 //   C[m][n] = sum over blocks b of 2^(ea[m][b] + eb[n][b]) * (sum over k in b of a[m][k] * b[n][k])
+//
+// v_mfma_scale_f32_16x16x128_f8f6f4 multiplies 16 x 128 by 128 x 16 codes and takes a power-of-two scale for
+// every row of either operand, so one block of 128 is one instruction with its scales, and the sum over
+// blocks stays in the fp32 accumulators.  A lane l gives 32 codes of row l % 16; which 32 of the 128 does not
+// matter as long as both operands agree, and all four lanes of a row give the same scale.
 #pragma once
 #include "packed.hip.h"
 
 namespace gtopk {
 
-// one value per thread, a block of 128 of sixteen rows of A and of B at a time in LDS
-template <class D>
-__global__ __launch_bounds__(256) void k_product(
-        const uint8_t* __restrict__ a, int64_t a_stride, const uint8_t* __restrict__ a_scales, int64_t a_scale_stride,
-        const uint8_t* __restrict__ b, int64_t b_stride, const uint8_t* __restrict__ b_scales, int64_t b_scale_stride,
-        int64_t M, int64_t N, uint32_t nb, typename D::T* __restrict__ out, int64_t out_stride, uint32_t tiles_n, uint64_t tiles) {
-    __shared__ float s_a[16][kPackBlock + 1], s_b[16][kPackBlock + 1];
-    const uint32_t r = threadIdx.x / 16, l = threadIdx.x % 16;
-    for (uint64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-        const int64_t m0 = (int64_t)(tile / tiles_n) * 16, n0 = (int64_t)(tile % tiles_n) * 16;
-        float sum = 0.0f;
-        for (uint32_t kb = 0; kb < nb; ++kb) {
-            float v[kLaneVals] = {}, w[kLaneVals] = {};
-            const int64_t col = (int64_t)kb * kPackBlock + l * kLaneVals;
-            if (m0 + r < M)
-                decode8(*reinterpret_cast<const uint32x2*>(a + (m0 + r) * a_stride + col), scale_value(a_scales[(m0 + r) * a_scale_stride + kb]), v);
-            if (n0 + r < N)
-                decode8(*reinterpret_cast<const uint32x2*>(b + (n0 + r) * b_stride + col), scale_value(b_scales[(n0 + r) * b_scale_stride + kb]), w);
+typedef int intx8 __attribute__((ext_vector_type(8)));
+typedef int intx4 __attribute__((ext_vector_type(4)));
+
+// The instruction for e4m3 numbers lines up the eight products of consecutive k with the largest of them and keeps 13 bits
+// below its leading one (measured: 2^-13 of it is added, 2^-14 lost; the sums of eight, and they with the accumulator, add
+// as fp32 numbers).  A 16-bit result is rounded to 2^-9 or 2^-12 of itself, more than that.  A result in fp32
+// is not, so there the codes are decoded to bf16 numbers, which hold them and their scales exactly, and multiplied at half the
+// rate by the instruction for those, which keeps 23 bits.
+template <class D> struct Exact { static constexpr bool value = false; };
+template <> struct Exact<F32> { static constexpr bool value = true; };
+
+struct PackedMatrix {
+    const uint8_t* codes;
+    const uint8_t* scales;
+    uint32_t code_stride, scale_stride;     // bytes
+};
+
+// 16 bytes per lane from global memory into LDS, lane l to `to` + 16 l (`to` is uniform)
+__device__ __forceinline__ void load_to_lds16(const uint8_t* from, uint8_t* to) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+}
+__device__ __forceinline__ void load_to_lds4(const uint8_t* from, uint8_t* to) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 4, 0, 0);
+}
+
+// 8 codes as bf16 numbers, exactly
+__device__ __forceinline__ bf16x8 decode_bf16(int c0, int c1, float scale) {
+    uint32x4 u;
+    u[0] = decode2<false>((uint32_t)c0, scale);
+    u[1] = decode2<true>((uint32_t)c0, scale);
+    u[2] = decode2<false>((uint32_t)c1, scale);
+    u[3] = decode2<true>((uint32_t)c1, scale);
+    return __builtin_bit_cast(bf16x8, u);
+}
+
+// Number `id` of `count` so that the ids that one XCD gets (id % 8, blocks are dealt out in turn) are consecutive numbers
+__device__ __forceinline__ uint32_t by_xcd(uint32_t id, uint32_t count) {
+    const uint32_t xcd = id % 8, each = count / 8, more = count % 8;
+    return xcd * each + (xcd < more ? xcd : more) + id / 8;
+}
+
+// A block computes BM x BN values with BM/WM x BN/WN waves of WM x WN each.  A block of 128 of the tile's rows of A and B
+// goes straight from global memory into one of two LDS buffers while the matrix instructions work on the other.
+// In LDS a row's 16-byte pieces are exchanged by the row's number (piece p lies at p ^ (row % 8)): rows are 128
+// bytes apart, and without that a wave's lanes would read from an eighth of the banks.  Rows behind the
+// matrix's end are read as its last row and not written.
+template <class D, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__((BM / WM) * (BN / WN) * kWave, 1) void k_product(
+        PackedMatrix a, PackedMatrix b, int64_t M, int64_t N, uint32_t nb, typename D::T* __restrict__ out, int64_t out_stride,
+        uint32_t tiles_m, uint32_t tiles_n) {
+    constexpr int kWavesN = BN / WN, kWaves = (BM / WM) * kWavesN, kThreads = kWaves * kWave;
+    constexpr int TM = WM / 16, TN = WN / 16;
+    constexpr bool kExact = Exact<D>::value;
+    constexpr int kStage = (BM + BN) * kPackBlock;
+    constexpr int kLoads = kStage / 16 / kThreads;                 // 16-byte pieces per thread and stage
+    static_assert(kStage % (16 * kThreads) == 0 && BM % (kThreads / 8) == 0, "whole loads, none of which has rows of both matrices");
+    __shared__ __align__(128) uint8_t s_codes[2][kStage];
+    __shared__ __align__(16) uint32_t s_scales[2][BM + BN];        // four blocks' scales of every row
+
+    const uint32_t wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+    const uint32_t tile = by_xcd(blockIdx.x, tiles_m * tiles_n);
+    const int64_t m0 = (int64_t)(tile % tiles_m) * BM, n0 = (int64_t)(tile / tiles_m) * BN;
+    const uint8_t* const a_base = a.codes + m0 * a.code_stride;
+    const uint8_t* const b_base = b.codes + n0 * b.code_stride;
+    const uint32_t a_last = (uint32_t)(M - m0 < BM ? M - m0 - 1 : BM - 1), b_last = (uint32_t)(N - n0 < BN ? N - n0 - 1 : BN - 1);
+
+    uint32_t offset[kLoads];
 #pragma unroll
-            for (int j = 0; j < kLaneVals; ++j) {
-                s_a[r][l * kLaneVals + j] = v[j];
-                s_b[r][l * kLaneVals + j] = w[j];
-            }
-            __syncthreads();
-            for (int k = 0; k < kPackBlock; ++k) sum += s_a[r][k] * s_b[l][k];
-            __syncthreads();
+    for (int i = 0; i < kLoads; ++i) {
+        const uint32_t r = (i * kThreads + threadIdx.x) / 8, piece = (threadIdx.x % 8) ^ (r % 8);
+        const bool of_a = i * kThreads / 8 < BM;
+        const uint32_t row = of_a ? (r < a_last ? r : a_last) : (r - BM < b_last ? r - BM : b_last);
+        offset[i] = row * (of_a ? a.code_stride : b.code_stride) + piece * 16;
+    }
+    auto fetch = [&](uint32_t kb, int buf) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const uint8_t* base = (i * kThreads / 8 < BM ? a_base : b_base) + (int64_t)kb * kPackBlock;
+            load_to_lds16(base + offset[i], s_codes[buf] + (i * kThreads + wave * kWave) * 16);
         }
-        if (m0 + r < M && n0 + l < N) out[(m0 + r) * out_stride + n0 + l] = (typename D::T)sum;
+    };
+    // four blocks' scales at a time; a row's scales can be read in fours to the end
+    auto fetch_scales = [&](uint32_t kb, int buf) {
+#pragma unroll
+        for (int i = 0; i < (BM + BN + kThreads - 1) / kThreads; ++i) {
+            const uint32_t r = i * kThreads + threadIdx.x;
+            if ((BM + BN) % kThreads == 0 || i * kThreads + wave * kWave < BM + BN) {
+                const bool of_a = r < BM;
+                const int64_t row = of_a ? m0 + (r < a_last ? r : a_last) : n0 + (r - BM < b_last ? r - BM : b_last);
+                load_to_lds4((of_a ? a.scales + row * a.scale_stride : b.scales + row * b.scale_stride) + kb,
+                             (uint8_t*)(s_scales[buf] + i * kThreads + wave * kWave));
+            }
+        }
+    };
+
+    const uint32_t wm = (wave / kWavesN) * WM, wn = (wave % kWavesN) * WN;
+    const uint32_t in16 = lane % 16, quarter = lane / 16;
+    // the lane's two pieces of a row: the row's number modulo 8 is in16 % 8 in every subtile
+    const uint32_t piece0 = ((2 * quarter) ^ (in16 % 8)) * 16, piece1 = ((2 * quarter + 1) ^ (in16 % 8)) * 16;
+    auto operand = [&](int buf, uint32_t row) {
+        const uint8_t* p = s_codes[buf] + (row + in16) * kPackBlock;
+        const intx4 lo = *reinterpret_cast<const intx4*>(p + piece0), hi = *reinterpret_cast<const intx4*>(p + piece1);
+        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+
+    floatx4 sum[TM][TN] = {};
+    uint32_t scale_a[TM], scale_b[TN];
+    fetch(0, 0);
+    fetch_scales(0, 0);
+    for (uint32_t kb = 0; kb < nb; ++kb) {
+        __syncthreads();                   // what was fetched is there; the other buffer has been read
+        const int buf = kb % 2;
+        if (kb % 4 == 0) {
+#pragma unroll
+            for (int i = 0; i < TM; ++i) scale_a[i] = s_scales[(kb / 4) % 2][wm + i * 16 + in16];
+#pragma unroll
+            for (int j = 0; j < TN; ++j) scale_b[j] = s_scales[(kb / 4) % 2][BM + wn + j * 16 + in16];
+        }
+        intx8 va[TM], vb[TN];
+#pragma unroll
+        for (int j = 0; j < TN; ++j) vb[j] = operand(buf, BM + wn + j * 16);
+#pragma unroll
+        for (int i = 0; i < TM; ++i) va[i] = operand(buf, wm + i * 16);
+        if (kb + 1 < nb) {
+            fetch(kb + 1, buf ^ 1);
+            if (kb % 4 == 3) fetch_scales(kb + 1, ((kb + 1) / 4) % 2);
+        }
+        // B is the instruction's first operand: a lane then holds four consecutive columns of C
+        if constexpr (kExact) {
+            float fa[TM], fb[TN];
+#pragma unroll
+            for (int i = 0; i < TM; ++i) fa[i] = scale_value(scale_a[i] & 255u);
+#pragma unroll
+            for (int j = 0; j < TN; ++j) fb[j] = scale_value(scale_b[j] & 255u);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                bf16x8 xa[TM], xb[TN];
+#pragma unroll
+                for (int j = 0; j < TN; ++j) xb[j] = decode_bf16(vb[j][2 * q], vb[j][2 * q + 1], fb[j]);
+#pragma unroll
+                for (int i = 0; i < TM; ++i) xa[i] = decode_bf16(va[i][2 * q], va[i][2 * q + 1], fa[i]);
+#pragma unroll
+                for (int i = 0; i < TM; ++i)
+#pragma unroll
+                    for (int j = 0; j < TN; ++j) sum[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xb[j], xa[i], sum[i][j], 0, 0, 0);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+                    sum[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(vb[j], va[i], sum[i][j], 0, 0, 0, (int)scale_b[j], 0, (int)scale_a[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < TM; ++i) scale_a[i] >>= 8;
+#pragma unroll
+        for (int j = 0; j < TN; ++j) scale_b[j] >>= 8;
+    }
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+        const int64_t m = m0 + wm + i * 16 + in16;
+        if (m >= M) continue;
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+            const int64_t n = n0 + wn + j * 16 + quarter * 4;
+            if (n < N) store4<D>(out + m * out_stride + n, N - n, sum[i][j]);
+        }
     }
 }
 

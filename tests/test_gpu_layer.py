@@ -279,6 +279,30 @@ def test_product_of_activations_and_weights(M, N, K):
     assert np.linalg.norm(err) <= 2.0 ** -17 * np.linalg.norm(va @ vb.T)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("M,N,K", [(1, 300, 5000), (20, 90, 1000), (70, 90, 1000), (257, 300, 1040), (300, 280, 2000)])
+def test_product_rounded_to_16_bits(M, N, K, dtype):
+    """Each of eight products of consecutive k loses less than 2^-13 of the largest one's leading bit, the sums of eight add
+    up in fp32, and the result is rounded once: 8 * 2^-13 of the largest of every eight, the fp32 sums' bound, half a step."""
+    import torch
+    from paper_1901_04359_amd import binding as B
+    t = torch_type(dtype)
+    a, b = ref.pack(values_in(M, K, 7)), ref.pack(values_in(N, K, 8) / math.sqrt(K), tiles=True)
+    va, vb = ref.values(*a, K), ref.values(*b, K)
+    out = torch.zeros(M, N, dtype=t, device="cuda")
+    say(f"layer: product {M}x{N}x{K} to {dtype}")
+    B.gtopk_scaled_product(*packed_on_gpu(*a), *packed_on_gpu(*b), K, out, B.alloc_product_workspace(M, N, K))
+    want = va @ vb.T
+    cut = np.zeros((M, N))
+    for k in range(0, K, 8):
+        cut += np.abs(va[:, None, k:k + 8] * vb[None, :, k:k + 8]).max(axis=2)
+    bound = 8 * 2.0 ** -13 * cut + (K + 4) * 2.0 ** -23 * (np.abs(va) @ np.abs(vb).T)
+    err = np.abs(out.double().cpu().numpy() - want)
+    assert (err <= bound * (1 + half_step(t)) + half_step(t) * np.abs(want) + (2.0 ** -25 if dtype == "f16" else 0.0)).all()
+    # the cut parts have both signs: in norm they stay below the rounding of either type
+    assert np.linalg.norm(err) <= 1.1 * half_step(t) * np.linalg.norm(want)
+
+
 @pytest.mark.parametrize("M,N,K", [(3, 40, 500), (130, 140, 300)])
 def test_product_with_nan_and_extreme_scales(M, N, K):
     """A NaN reaches its row or column and nothing else; scales at the ends of their range."""
