@@ -431,53 +431,85 @@ def gtopk_debug_candidate_counts(ws, m: int, k: int, P: int):
 # -- a layer in 8 bits ----------------------------------------------------------
 # codes and scales are torch.uint8 tensors ([rows][code_stride], [rows][scale_stride]; alloc_packed makes them);
 # dense matrices are 2-D float32, bfloat16 or float16 tensors with contiguous rows.  All tensors of a call lie on one
-# GPU, and the call runs there, on that GPU's current stream.
+# GPU, and the call runs there, on that GPU's current stream.  The smallest of these calls take a few
+# microseconds on the GPU, so the checks are written to cost less than that.
 
 ACTS = ("none", "relu", "tanh", "sigmoid", "silu", "gelu")
 PACK_BLOCK = 128
-
-
-def _dtype_code(t, name: str) -> int:
-    torch = _torch()
-    codes = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
-    if not isinstance(t, torch.Tensor) or t.dtype not in codes:
-        raise TypeError(f"{name} must be a float32, bfloat16 or float16 tensor")
-    return codes[t.dtype]
+_ACT_CODES = {name: i for i, name in enumerate(ACTS)}
 
 
 def _act_code(act: str) -> int:
-    if act not in ACTS:
+    code = _ACT_CODES.get(act)
+    if code is None:
         raise ValueError(f"act must be one of {ACTS}, got {act!r}")
-    return ACTS.index(act)
+    return code
 
 
-def _dense(t, name: str):
-    """(rows, cols, stride) of a dense 2-D matrix with contiguous rows."""
-    if t.dim() != 2 or t.shape[1] < 1 or (t.stride(1) != 1 and t.shape[1] > 1):
+def _gpu(t, torch, name: str) -> int:
+    """The number of the GPU that the tensor lies on."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a GPU tensor")
+    device = t.get_device()
+    if device < 0:
+        raise TypeError(f"{name} must be a GPU tensor")
+    return device
+
+
+def _dense(t, torch, name: str):
+    """(dtype code, rows, cols, stride) of a dense 2-D matrix with contiguous rows."""
+    dtype = t.dtype
+    code = 0 if dtype == torch.float32 else 1 if dtype == torch.bfloat16 else 2 if dtype == torch.float16 else -1
+    if code < 0:
+        raise TypeError(f"{name} must be a float32, bfloat16 or float16 tensor, got {dtype}")
+    if t.dim() != 2:
         raise ValueError(f"{name} must be 2-D with contiguous rows")
-    return t.shape[0], t.shape[1], (t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1]))
+    rows, cols = t.shape
+    stride, one = t.stride()
+    if cols < 1 or (one != 1 and cols > 1):
+        raise ValueError(f"{name} must be 2-D with contiguous rows")
+    return code, rows, cols, (stride if rows > 1 else max(stride, cols))
 
 
-def _packed(codes, scales, rows: int, cols: int, name: str):
+def _packed(codes, scales, rows: int, cols: int, torch, name: str):
     """(code_stride, scale_stride) of the packed matrix `name` that must hold rows x cols values."""
     nb = -(-cols // PACK_BLOCK)
+    strides = []
     for t, least, of, what in ((codes, nb * PACK_BLOCK, PACK_BLOCK, "codes"), (scales, nb, 4, "scales")):
-        if t.dim() != 2 or t.shape[0] != rows or t.shape[1] < least or (t.stride(1) != 1 and t.shape[1] > 1):
-            raise ValueError(f"{name}{what} must be 2-D with contiguous rows, {rows} rows of at least {least} bytes")
-        # the last row is read to its multiple, so it must be there
-        if t.shape[1] % of:
-            raise ValueError(f"{name}{what} must have a multiple of {of} columns")
-    stride = lambda t: t.stride(0) if rows > 1 else t.shape[1]
-    return stride(codes), stride(scales)
+        if t.dtype != torch.uint8:
+            raise TypeError(f"{name}{what} must have dtype torch.uint8, got {t.dtype}")
+        if t.dim() != 2:
+            raise ValueError(f"{name}{what} must be 2-D with contiguous rows")
+        have, width = t.shape
+        stride, one = t.stride()
+        # the last row, too, is read to its multiple
+        if have != rows or width < least or width % of or one != 1:
+            raise ValueError(f"{name}{what} must have {rows} contiguous rows of at least {least} bytes, a multiple of {of}")
+        strides.append(stride if rows > 1 else width)
+    return strides
 
 
-def _on_device(*tensors):
-    """A context in which the tensors' GPU is the current one; ValueError if they lie on several."""
-    torch = _torch()
-    devices = {t.device for t in tensors if isinstance(t, torch.Tensor)}
-    if len(devices) > 1:
-        raise ValueError(f"tensors lie on several devices: {sorted(map(str, devices))}")
-    return torch.cuda.device(devices.pop())
+def _workspace(ws, torch) -> int:
+    if ws.dtype != torch.uint8 or not ws.is_contiguous():
+        raise TypeError("ws must be a contiguous torch.uint8 tensor")
+    return ws.numel()
+
+
+def _run(name: str, torch, devices, *args) -> None:
+    """Calls an entry point on the tensors' GPU, with its current stream as the last argument."""
+    device = devices[0]
+    for other in devices:
+        if other != device:
+            raise ValueError(f"{name}: tensors lie on several GPUs: {sorted(set(devices))}")
+    f = getattr(_lib or load(), name)
+    stream = torch._C._cuda_getCurrentRawStream(device)
+    if device == torch.cuda.current_device():
+        rc = f(*args, stream)
+    else:
+        with torch.cuda.device(device):
+            rc = f(*args, stream)
+    if rc:
+        raise GtopkError(rc, name)
 
 
 def alloc_packed(rows: int, cols: int, device="cuda"):
@@ -490,60 +522,53 @@ def alloc_packed(rows: int, cols: int, device="cuda"):
 
 def gtopk_pack_rows(x, codes, scales) -> None:
     torch = _torch()
-    dtype = _dtype_code(x, "x")
-    rows, cols, stride = _dense(x, "x")
-    px, pc, ps = _ptr(x, x.dtype, "x"), _ptr(codes, torch.uint8, "codes"), _ptr(scales, torch.uint8, "scales")
-    code_stride, scale_stride = _packed(codes, scales, rows, cols, "")
-    with _on_device(x, codes, scales):
-        rc = load().gtopk_pack_rows(px, dtype, rows, cols, stride, pc, code_stride, ps, scale_stride, _stream())
-    _check(rc, "gtopk_pack_rows")
+    devices = (_gpu(x, torch, "x"), _gpu(codes, torch, "codes"), _gpu(scales, torch, "scales"))
+    dtype, rows, cols, stride = _dense(x, torch, "x")
+    code_stride, scale_stride = _packed(codes, scales, rows, cols, torch, "")
+    _run("gtopk_pack_rows", torch, devices, x.data_ptr(), dtype, rows, cols, stride, codes.data_ptr(), code_stride,
+         scales.data_ptr(), scale_stride)
 
 
 def gtopk_pack_tiles(x, codes=None, scales=None, codes_t=None, scales_t=None) -> None:
     """Either pair may be None, not both."""
     torch = _torch()
-    dtype = _dtype_code(x, "x")
-    rows, cols, stride = _dense(x, "x")
-    args = [_ptr(x, x.dtype, "x"), dtype, rows, cols, stride]
+    devices = [_gpu(x, torch, "x")]
+    dtype, rows, cols, stride = _dense(x, torch, "x")
+    args = []
     for c, s, shape, name in ((codes, scales, (rows, cols), ""), (codes_t, scales_t, (cols, rows), "transposed ")):
         if (c is None) != (s is None):
             raise ValueError(f"{name}codes and scales go together")
-        pc, ps = _ptr(c, torch.uint8, name + "codes", True), _ptr(s, torch.uint8, name + "scales", True)
-        if c is None or rows == 0:
-            args += [pc, 0, ps, 0]
-        else:
-            code_stride, scale_stride = _packed(c, s, *shape, name)
-            args += [pc, code_stride, ps, scale_stride]
-    with _on_device(x, codes, scales, codes_t, scales_t):
-        rc = load().gtopk_pack_tiles(*args, _stream())
-    _check(rc, "gtopk_pack_tiles")
+        if c is None:
+            args += (None, 0, None, 0)
+            continue
+        devices += (_gpu(c, torch, name + "codes"), _gpu(s, torch, name + "scales"))
+        code_stride, scale_stride = _packed(c, s, *shape, torch, name) if rows else (0, 0)
+        args += (c.data_ptr(), code_stride, s.data_ptr(), scale_stride)
+    _run("gtopk_pack_tiles", torch, devices, x.data_ptr(), dtype, rows, cols, stride, *args)
 
 
 def gtopk_unpack(codes, scales, act: str, out) -> None:
     torch = _torch()
-    dtype = _dtype_code(out, "out")
-    rows, cols, stride = _dense(out, "out")
-    pc, ps, po = _ptr(codes, torch.uint8, "codes"), _ptr(scales, torch.uint8, "scales"), _ptr(out, out.dtype, "out")
-    code_stride, scale_stride = _packed(codes, scales, rows, cols, "")
-    with _on_device(codes, scales, out):
-        rc = load().gtopk_unpack(pc, code_stride, ps, scale_stride, rows, cols, _act_code(act), po, dtype, stride, _stream())
-    _check(rc, "gtopk_unpack")
+    devices = (_gpu(codes, torch, "codes"), _gpu(scales, torch, "scales"), _gpu(out, torch, "out"))
+    dtype, rows, cols, stride = _dense(out, torch, "out")
+    code_stride, scale_stride = _packed(codes, scales, rows, cols, torch, "")
+    _run("gtopk_unpack", torch, devices, codes.data_ptr(), code_stride, scales.data_ptr(), scale_stride, rows, cols,
+         _act_code(act), out.data_ptr(), dtype, stride)
 
 
 def gtopk_activation_grad(codes, scales, act: str, dy, dx) -> None:
     """dx may be dy."""
     torch = _torch()
-    dtype = _dtype_code(dy, "dy")
-    rows, cols, dy_stride = _dense(dy, "dy")
-    if _dense(dx, "dx")[:2] != (rows, cols):
+    devices = (_gpu(codes, torch, "codes"), _gpu(scales, torch, "scales"), _gpu(dy, torch, "dy"), _gpu(dx, torch, "dx"))
+    dtype, rows, cols, dy_stride = _dense(dy, torch, "dy")
+    dx_dtype, dx_rows, dx_cols, dx_stride = _dense(dx, torch, "dx")
+    if (dx_rows, dx_cols) != (rows, cols):
         raise ValueError("dy and dx must have the same shape")
-    pc, ps = _ptr(codes, torch.uint8, "codes"), _ptr(scales, torch.uint8, "scales")
-    pd, px = _ptr(dy, dy.dtype, "dy"), _ptr(dx, dy.dtype, "dx")
-    code_stride, scale_stride = _packed(codes, scales, rows, cols, "")
-    with _on_device(codes, scales, dy, dx):
-        rc = load().gtopk_activation_grad(pc, code_stride, ps, scale_stride, rows, cols, _act_code(act), pd, dy_stride, px,
-                                          _dense(dx, "dx")[2], dtype, _stream())
-    _check(rc, "gtopk_activation_grad")
+    if dx_dtype != dtype:
+        raise TypeError("dy and dx must have the same dtype")
+    code_stride, scale_stride = _packed(codes, scales, rows, cols, torch, "")
+    _run("gtopk_activation_grad", torch, devices, codes.data_ptr(), code_stride, scales.data_ptr(), scale_stride, rows, cols,
+         _act_code(act), dy.data_ptr(), dy_stride, dx.data_ptr(), dx_stride, dtype)
 
 
 def gtopk_product_workspace_bytes(M: int, N: int, K: int) -> int:
@@ -561,18 +586,16 @@ def alloc_product_workspace(M: int, N: int, K: int, device="cuda"):
 def gtopk_scaled_product(a_codes, a_scales, b_codes, b_scales, K: int, out, ws) -> None:
     """out [M][N] = A B^T for packed A (M x K) and B (N x K)."""
     torch = _torch()
-    dtype = _dtype_code(out, "out")
-    M, N, stride = _dense(out, "out")
-    pa, pas = _ptr(a_codes, torch.uint8, "a_codes"), _ptr(a_scales, torch.uint8, "a_scales")
-    pb, pbs = _ptr(b_codes, torch.uint8, "b_codes"), _ptr(b_scales, torch.uint8, "b_scales")
-    po, pw = _ptr(out, out.dtype, "out"), _ptr(ws, torch.uint8, "ws")
+    devices = (_gpu(a_codes, torch, "a_codes"), _gpu(a_scales, torch, "a_scales"), _gpu(b_codes, torch, "b_codes"),
+               _gpu(b_scales, torch, "b_scales"), _gpu(out, torch, "out"), _gpu(ws, torch, "ws"))
     if K < 1:
         raise ValueError("K must be at least 1")
-    a_strides, b_strides = _packed(a_codes, a_scales, M, K, "a_"), _packed(b_codes, b_scales, N, K, "b_")
-    with _on_device(a_codes, a_scales, b_codes, b_scales, out, ws):
-        rc = load().gtopk_scaled_product(pa, a_strides[0], pas, a_strides[1], pb, b_strides[0], pbs, b_strides[1], M, N, K,
-                                         po, dtype, stride, pw, ws.numel(), _stream())
-    _check(rc, "gtopk_scaled_product")
+    dtype, M, N, stride = _dense(out, torch, "out")
+    a_stride, as_stride = _packed(a_codes, a_scales, M, K, torch, "a_")
+    b_stride, bs_stride = _packed(b_codes, b_scales, N, K, torch, "b_")
+    _run("gtopk_scaled_product", torch, devices, a_codes.data_ptr(), a_stride, a_scales.data_ptr(), as_stride,
+         b_codes.data_ptr(), b_stride, b_scales.data_ptr(), bs_stride, M, N, K, out.data_ptr(), dtype, stride,
+         ws.data_ptr(), _workspace(ws, torch))
 
 
 def gtopk_weight_grad_workspace_bytes(rows: int, P: int, N: int, K: int) -> int:
@@ -591,20 +614,26 @@ def gtopk_weight_grad(dy, codes, scales, row_begin, grad, accumulate: bool, ws) 
     """grad: float32 [P][N][K], for example grads[:, at:at + N*K].unflatten(1, (N, K)) of the workers' gradient rows;
     row_begin: int32 [P + 1] on the GPU, or None for equal shares."""
     torch = _torch()
-    dtype = _dtype_code(dy, "dy")
-    rows, N, dy_stride = _dense(dy, "dy")
+    devices = [_gpu(dy, torch, "dy"), _gpu(codes, torch, "codes"), _gpu(scales, torch, "scales"), _gpu(grad, torch, "grad"),
+               _gpu(ws, torch, "ws")]
+    dtype, rows, N, dy_stride = _dense(dy, torch, "dy")
+    if grad.dtype != torch.float32:
+        raise TypeError(f"grad must have dtype torch.float32, got {grad.dtype}")
     if grad.dim() != 3 or grad.shape[1] != N or grad.shape[0] < 1 or grad.shape[2] < 1:
         raise ValueError("grad must be [P][N][K], with as many rows as dy has columns")
     P, _, K = grad.shape
-    if (K > 1 and grad.stride(2) != 1) or (N > 1 and grad.stride(1) != K):
+    p_stride, n_stride, k_stride = grad.stride()
+    if (K > 1 and k_stride != 1) or (N > 1 and n_stride != K):
         raise ValueError("grad must hold each worker's N x K weights contiguously")
-    pd, pc, ps = _ptr(dy, dy.dtype, "dy"), _ptr(codes, torch.uint8, "codes"), _ptr(scales, torch.uint8, "scales")
-    pb = _ptr(row_begin, torch.int32, "row_begin", allow_none=True)
-    if row_begin is not None and (row_begin.dim() != 1 or row_begin.numel() != P + 1 or row_begin.stride(0) != 1):
-        raise ValueError("row_begin must hold P + 1 entries")
-    pg, pw = _ptr(grad, torch.float32, "grad"), _ptr(ws, torch.uint8, "ws")
-    code_stride, scale_stride = _packed(codes, scales, rows, K, "")
-    with _on_device(dy, codes, scales, row_begin, grad, ws):
-        rc = load().gtopk_weight_grad(pd, dtype, dy_stride, pc, code_stride, ps, scale_stride, rows, pb, P, N, K, pg,
-                                      grad.stride(0) if P > 1 else N * K, 1 if accumulate else 0, pw, ws.numel(), _stream())
-    _check(rc, "gtopk_weight_grad")
+    begin = None
+    if row_begin is not None:
+        devices.append(_gpu(row_begin, torch, "row_begin"))
+        if row_begin.dtype != torch.int32:
+            raise TypeError(f"row_begin must have dtype torch.int32, got {row_begin.dtype}")
+        if row_begin.dim() != 1 or row_begin.numel() != P + 1 or row_begin.stride(0) != 1:
+            raise ValueError("row_begin must hold P + 1 entries")
+        begin = row_begin.data_ptr()
+    code_stride, scale_stride = _packed(codes, scales, rows, K, torch, "")
+    _run("gtopk_weight_grad", torch, devices, dy.data_ptr(), dtype, dy_stride, codes.data_ptr(), code_stride,
+         scales.data_ptr(), scale_stride, rows, begin, P, N, K, grad.data_ptr(), p_stride if P > 1 else N * K,
+         1 if accumulate else 0, ws.data_ptr(), _workspace(ws, torch))

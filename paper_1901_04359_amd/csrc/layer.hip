@@ -15,6 +15,7 @@ using namespace gtopk;
 namespace {
 
 constexpr int64_t kMaxSide = 0x7FFFFFFF;            // rows and columns of a matrix
+constexpr int64_t kThinRows = 64;                   // products with at most so many rows of A: k_product_thin
 constexpr int64_t kMaxCodeStride = 1 << 23;         // of a product's operands: a tile's rows at offsets of 32 bits
 constexpr uint64_t kMaxBlocks = 1u << 22;           // blocks of a launch; kernels walk what is left
 
@@ -173,15 +174,25 @@ int gtopk_scaled_product(const uint8_t* a_codes, int64_t a_code_stride, const ui
     if (ws_bytes < need) return GTOPK_EWORKSPACE;
     const PackedMatrix a{a_codes, a_scales, (uint32_t)a_code_stride, (uint32_t)a_scale_stride};
     const PackedMatrix b{b_codes, b_scales, (uint32_t)b_code_stride, (uint32_t)b_scale_stride};
+    const uint32_t nb = (uint32_t)ceil_div(K, kPackBlock);
+    hipStream_t st = (hipStream_t)stream;
     by_type(dtype, [&](auto d) {
         using D = decltype(d);
+        typename D::T* const to = (typename D::T*)out;
+        if (M <= kThinRows) {
+            const dim3 grid((uint32_t)ceil_div(N, 16)), block(kThinWaves * kWave);
+            if (M <= 16) hipLaunchKernelGGL((k_product_thin<D, 1>), grid, block, 0, st, a, b, M, N, nb, to, out_stride);
+            else if (M <= 32) hipLaunchKernelGGL((k_product_thin<D, 2>), grid, block, 0, st, a, b, M, N, nb, to, out_stride);
+            else hipLaunchKernelGGL((k_product_thin<D, 4>), grid, block, 0, st, a, b, M, N, nb, to, out_stride);
+            return;
+        }
 #ifndef CFG
 #define CFG 128, 128, 64, 64
 #endif
         constexpr int c[4] = {CFG};
         const uint32_t tiles_m = (uint32_t)ceil_div(M, c[0]), tiles_n = (uint32_t)ceil_div(N, c[1]);
         hipLaunchKernelGGL((k_product<D, CFG>), dim3(tiles_m * tiles_n), dim3((c[0] / c[2]) * (c[1] / c[3]) * kWave), 0,
-                           (hipStream_t)stream, a, b, M, N, (uint32_t)ceil_div(K, kPackBlock), (typename D::T*)out, out_stride, tiles_m, tiles_n);
+                           st, a, b, M, N, nb, to, out_stride, tiles_m, tiles_n);
     });
     return launch_status();
 }

@@ -45,6 +45,20 @@ __device__ __forceinline__ bf16x8 decode_bf16(int c0, int c1, float scale) {
     return __builtin_bit_cast(bf16x8, u);
 }
 
+// sum + one block of 128: B's row is the instruction's first operand, so a lane holds four consecutive columns of C
+template <class D>
+__device__ __forceinline__ floatx4 multiply(intx8 vb, uint32_t sb, intx8 va, uint32_t sa, floatx4 sum) {
+    if constexpr (Exact<D>::value) {
+        const float fa = scale_value(sa), fb = scale_value(sb);
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode_bf16(vb[2 * q], vb[2 * q + 1], fb), decode_bf16(va[2 * q], va[2 * q + 1], fa), sum, 0, 0, 0);
+        return sum;
+    } else {
+        return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(vb, va, sum, 0, 0, 0, (int)sb, 0, (int)sa);
+    }
+}
+
 // Number `id` of `count` so that the ids that one XCD gets (id % 8, blocks are dealt out in turn) are consecutive numbers
 __device__ __forceinline__ uint32_t by_xcd(uint32_t id, uint32_t count) {
     const uint32_t xcd = id % 8, each = count / 8, more = count % 8;
@@ -177,6 +191,67 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * kWave, 1) void k_product(
             const int64_t n = n0 + wn + j * 16 + quarter * 4;
             if (n < N) store4<D>(out + m * out_stride + n, N - n, sum[i][j]);
         }
+    }
+}
+
+// Few rows of A (at most 16 TM): what counts is reading B once at the memory's rate.  A block computes 16 columns of C
+// with kThinWaves waves that share out the blocks of 128 among them and read both matrices straight into registers, kThinAhead
+// blocks of 128 at a time, so that a compute unit has some 64 KB of B under way; the waves' sums are joined in LDS, in their order.
+constexpr int kThinWaves = 8;
+constexpr int kThinAhead = 4;
+template <class D, int TM>
+__global__ __launch_bounds__(kThinWaves * kWave) void k_product_thin(PackedMatrix a, PackedMatrix b, int64_t M, int64_t N, uint32_t nb,
+                                                                   typename D::T* __restrict__ out, int64_t out_stride) {
+    constexpr int kAhead = TM > 1 ? kThinAhead / 2 : kThinAhead;
+    __shared__ floatx4 s_sum[kThinWaves][TM][kWave];
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, in16 = lane % 16, quarter = lane / 16;
+    const int64_t n0 = (int64_t)blockIdx.x * 16;
+    const int64_t n = n0 + in16 < N ? n0 + in16 : N - 1;
+    const uint8_t* const b_row = b.codes + n * b.code_stride + quarter * 32;
+    const uint8_t* const b_scale = b.scales + n * b.scale_stride;
+    const uint8_t *a_row[TM], *a_scale[TM];
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+        const int64_t m = i * 16 + in16 < M ? i * 16 + in16 : M - 1;
+        a_row[i] = a.codes + m * a.code_stride + quarter * 32;
+        a_scale[i] = a.scales + m * a.scale_stride;
+    }
+    auto codes = [](const uint8_t* p) {
+        const intx4 lo = *reinterpret_cast<const intx4*>(p), hi = *reinterpret_cast<const intx4*>(p + 16);
+        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+    floatx4 sum[TM] = {};
+    for (uint32_t k0 = wave; k0 < nb; k0 += kThinWaves * kAhead) {
+        intx8 va[kAhead][TM], vb[kAhead];
+        uint32_t sa[kAhead][TM], sb[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {         // behind the last block the last one once more, which is not used
+            const uint32_t kb = k0 + u * kThinWaves < nb ? k0 + u * kThinWaves : nb - 1;
+            vb[u] = codes(b_row + (uint64_t)kb * kPackBlock);
+            sb[u] = b_scale[kb];
+#pragma unroll
+            for (int i = 0; i < TM; ++i) {
+                va[u][i] = codes(a_row[i] + (uint64_t)kb * kPackBlock);
+                sa[u][i] = a_scale[i][kb];
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            if (k0 + u * kThinWaves < nb) {
+#pragma unroll
+                for (int i = 0; i < TM; ++i) sum[i] = multiply<D>(vb[u], sb[u], va[u][i], sa[u][i], sum[i]);
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < TM; ++i) s_sum[wave][i][lane] = sum[i];
+    __syncthreads();
+    for (int i = wave; i < TM; i += kThinWaves) {
+        floatx4 v = s_sum[0][i][lane];
+#pragma unroll
+        for (int w = 1; w < kThinWaves; ++w) v += s_sum[w][i][lane];
+        const int64_t m = i * 16 + in16, at = n0 + quarter * 4;
+        if (m < M && at < N) store4<D>(out + m * out_stride + at, N - at, v);
     }
 }
 

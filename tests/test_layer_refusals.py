@@ -106,13 +106,13 @@ def test_binding_refusals():
     with pytest.raises(ValueError):
         B._act_code("softmax")
     with pytest.raises(ValueError):
-        B._packed(u, torch.zeros(4, 2, dtype=torch.uint8), 4, 130, "")      # scales not in fours
+        B._packed(u, torch.zeros(4, 2, dtype=torch.uint8), 4, 130, torch, "")      # scales not in fours
     with pytest.raises(ValueError):
-        B._packed(u, torch.zeros(4, 4, dtype=torch.uint8), 4, 257, "")      # too few codes
+        B._packed(u, torch.zeros(4, 4, dtype=torch.uint8), 4, 257, torch, "")      # too few codes
     with pytest.raises(ValueError):
-        B._packed(u, torch.zeros(3, 4, dtype=torch.uint8), 4, 130, "")      # another number of rows
+        B._packed(u, torch.zeros(3, 4, dtype=torch.uint8), 4, 130, torch, "")      # another number of rows
     with pytest.raises(ValueError):
-        B._dense(x.t(), "x")
+        B._dense(x.t(), torch, "x")
     with pytest.raises(B.GtopkError):
         B.alloc_product_workspace(4, 0, 4)
     with pytest.raises(B.GtopkError):
