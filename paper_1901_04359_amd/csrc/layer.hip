@@ -191,7 +191,7 @@ int gtopk_scaled_product(const uint8_t* a_codes, int64_t a_code_stride, const ui
 #endif
         constexpr int c[4] = {CFG};
         const uint32_t tiles_m = (uint32_t)ceil_div(M, c[0]), tiles_n = (uint32_t)ceil_div(N, c[1]);
-        hipLaunchKernelGGL((k_product<D, CFG>), dim3(tiles_m * tiles_n), dim3((c[0] / c[2]) * (c[1] / c[3]) * kWave), 0,
+        hipLaunchKernelGGL((k_product<D, Exact<D>::value, CFG>), dim3(tiles_m * tiles_n), dim3((c[0] / c[2]) * (c[1] / c[3]) * kWave), 0,
                            st, a, b, M, N, nb, to, out_stride, tiles_m, tiles_n);
     });
     return launch_status();

@@ -46,10 +46,10 @@ __device__ __forceinline__ bf16x8 decode_bf16(int c0, int c1, float scale) {
 }
 
 // sum + one block of 128: B's row is the instruction's first operand, so a lane holds four consecutive columns of C
-template <class D>
+template <bool EXACT>
 __device__ __forceinline__ floatx4 multiply(intx8 vb, uint32_t sb, intx8 va, uint32_t sa, floatx4 sum) {
-    if constexpr (Exact<D>::value) {
-        const float fa = scale_value(sa), fb = scale_value(sb);
+    if constexpr (EXACT) {
+        const float fa = scale_value(sa & 255u), fb = scale_value(sb & 255u);
 #pragma unroll
         for (int q = 0; q < 4; ++q)
             sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode_bf16(vb[2 * q], vb[2 * q + 1], fb), decode_bf16(va[2 * q], va[2 * q + 1], fa), sum, 0, 0, 0);
@@ -65,27 +65,41 @@ __device__ __forceinline__ uint32_t by_xcd(uint32_t id, uint32_t count) {
     return xcd * each + (xcd < more ? xcd : more) + id / 8;
 }
 
+// tile `t` of tiles_m x tiles_n: columns of `high` tiles, one column of tiles after the other, so that the tiles that are
+// worked on side by side are about as many down as across and share their rows of A and B in an XCD's L2
+__device__ __forceinline__ void tile_at(uint32_t t, uint32_t tiles_m, uint32_t tiles_n, uint32_t high, uint32_t& m, uint32_t& n) {
+    const uint32_t band = t / (high * tiles_n), first = band * high, in = t - band * high * tiles_n;
+    const uint32_t rows = tiles_m - first < high ? tiles_m - first : high;
+    m = first + in % rows;
+    n = in / rows;
+}
+
 // A block computes BM x BN values with BM/WM x BN/WN waves of WM x WN each.  A block of 128 of the tile's rows of A and B
-// goes straight from global memory into one of two LDS buffers while the matrix instructions work on the other.
-// In LDS a row's 16-byte pieces are exchanged by the row's number (piece p lies at p ^ (row % 8)): rows are 128
+// goes straight from global memory into one of two LDS buffers while the matrix instructions work on the other; the scales
+// of four blocks go together (a word per row: fetched one by one they would be as many requests as the codes).
+// In LDS a row's 16-byte pieces are exchanged by the row's number (piece p lies at p ^ (row / 2 % 8)): rows are 128
 // bytes apart, and without that a wave's lanes would read from an eighth of the banks.  Rows behind the
 // matrix's end are read as its last row and not written.
-template <class D, int BM, int BN, int WM, int WN>
+template <class D, bool EXACT, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__((BM / WM) * (BN / WN) * kWave, 1) void k_product(
         PackedMatrix a, PackedMatrix b, int64_t M, int64_t N, uint32_t nb, typename D::T* __restrict__ out, int64_t out_stride,
         uint32_t tiles_m, uint32_t tiles_n) {
     constexpr int kWavesN = BN / WN, kWaves = (BM / WM) * kWavesN, kThreads = kWaves * kWave;
     constexpr int TM = WM / 16, TN = WN / 16;
-    constexpr bool kExact = Exact<D>::value;
+    constexpr int kScaleLoads = (BM + BN + kThreads - 1) / kThreads;
     constexpr int kStage = (BM + BN) * kPackBlock;
     constexpr int kLoads = kStage / 16 / kThreads;                 // 16-byte pieces per thread and stage
     static_assert(kStage % (16 * kThreads) == 0 && BM % (kThreads / 8) == 0, "whole loads, none of which has rows of both matrices");
-    __shared__ __align__(128) uint8_t s_codes[2][kStage];
-    __shared__ __align__(16) uint32_t s_scales[2][BM + BN];        // four blocks' scales of every row
+    // arrays of their own, so that the compiler can tell a load into one from a read of another
+    __shared__ __align__(128) uint8_t s_codes0[kStage];
+    __shared__ __align__(128) uint8_t s_codes1[kStage];
+    __shared__ __align__(128) uint8_t s_scales[2][kScaleLoads * kThreads * 4];      // a word per row: four blocks' scales
 
     const uint32_t wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
     const uint32_t tile = by_xcd(blockIdx.x, tiles_m * tiles_n);
-    const int64_t m0 = (int64_t)(tile % tiles_m) * BM, n0 = (int64_t)(tile / tiles_m) * BN;
+    uint32_t tile_m, tile_n;
+    tile_at(tile, tiles_m, tiles_n, 2048 / BM, tile_m, tile_n);
+    const int64_t m0 = (int64_t)tile_m * BM, n0 = (int64_t)tile_n * BN;
     const uint8_t* const a_base = a.codes + m0 * a.code_stride;
     const uint8_t* const b_base = b.codes + n0 * b.code_stride;
     const uint32_t a_last = (uint32_t)(M - m0 < BM ? M - m0 - 1 : BM - 1), b_last = (uint32_t)(N - n0 < BN ? N - n0 - 1 : BN - 1);
@@ -93,95 +107,78 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * kWave, 1) void k_product(
     uint32_t offset[kLoads];
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-        const uint32_t r = (i * kThreads + threadIdx.x) / 8, piece = (threadIdx.x % 8) ^ (r % 8);
+        const uint32_t r = (i * kThreads + threadIdx.x) / 8, piece = (threadIdx.x % 8) ^ (r / 2 % 8);
         const bool of_a = i * kThreads / 8 < BM;
         const uint32_t row = of_a ? (r < a_last ? r : a_last) : (r - BM < b_last ? r - BM : b_last);
         offset[i] = row * (of_a ? a.code_stride : b.code_stride) + piece * 16;
     }
-    auto fetch = [&](uint32_t kb, int buf) {
+    // (a row's scales can be read in fours to the end)
+    const uint8_t* scales_from[kScaleLoads];
+#pragma unroll
+    for (int i = 0; i < kScaleLoads; ++i) {
+        const uint32_t r = i * kThreads + threadIdx.x;
+        scales_from[i] = r < BM ? a.scales + (m0 + (r < a_last ? r : a_last)) * a.scale_stride
+                                : b.scales + (n0 + (r - BM < b_last ? r - BM : b_last)) * b.scale_stride;
+    }
+    auto fetch = [&](uint32_t kb, uint8_t* stage) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             const uint8_t* base = (i * kThreads / 8 < BM ? a_base : b_base) + (int64_t)kb * kPackBlock;
-            load_to_lds16(base + offset[i], s_codes[buf] + (i * kThreads + wave * kWave) * 16);
+            load_to_lds16(base + offset[i], stage + (i * kThreads + wave * kWave) * 16);
         }
     };
-    // four blocks' scales at a time; a row's scales can be read in fours to the end
-    auto fetch_scales = [&](uint32_t kb, int buf) {
+    auto fetch_scales = [&](uint32_t kb, uint8_t* to) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < (BM + BN + kThreads - 1) / kThreads; ++i) {
-            const uint32_t r = i * kThreads + threadIdx.x;
-            if ((BM + BN) % kThreads == 0 || i * kThreads + wave * kWave < BM + BN) {
-                const bool of_a = r < BM;
-                const int64_t row = of_a ? m0 + (r < a_last ? r : a_last) : n0 + (r - BM < b_last ? r - BM : b_last);
-                load_to_lds4((of_a ? a.scales + row * a.scale_stride : b.scales + row * b.scale_stride) + kb,
-                             (uint8_t*)(s_scales[buf] + i * kThreads + wave * kWave));
-            }
-        }
+        for (int i = 0; i < kScaleLoads; ++i) load_to_lds4(scales_from[i] + kb, to + (i * kThreads + wave * kWave) * 4);
     };
 
     const uint32_t wm = (wave / kWavesN) * WM, wn = (wave % kWavesN) * WN;
     const uint32_t in16 = lane % 16, quarter = lane / 16;
-    // the lane's two pieces of a row: the row's number modulo 8 is in16 % 8 in every subtile
-    const uint32_t piece0 = ((2 * quarter) ^ (in16 % 8)) * 16, piece1 = ((2 * quarter + 1) ^ (in16 % 8)) * 16;
-    auto operand = [&](int buf, uint32_t row) {
-        const uint8_t* p = s_codes[buf] + (row + in16) * kPackBlock;
+    // the lane's two pieces of a row (of which the subtiles' first row is a multiple of 16)
+    const uint32_t piece0 = in16 * kPackBlock + ((2 * quarter) ^ (in16 / 2)) * 16, piece1 = in16 * kPackBlock + ((2 * quarter + 1) ^ (in16 / 2)) * 16;
+    auto operand = [&](const uint8_t* stage, uint32_t row) __attribute__((always_inline)) {
+        const uint8_t* p = stage + row * kPackBlock;
         const intx4 lo = *reinterpret_cast<const intx4*>(p + piece0), hi = *reinterpret_cast<const intx4*>(p + piece1);
         return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     };
 
     floatx4 sum[TM][TN] = {};
-    uint32_t scale_a[TM], scale_b[TN];
-    fetch(0, 0);
-    fetch_scales(0, 0);
-    for (uint32_t kb = 0; kb < nb; ++kb) {
-        __syncthreads();                   // what was fetched is there; the other buffer has been read
-        const int buf = kb % 2;
-        if (kb % 4 == 0) {
+    uint32_t sa[TM], sb[TN];
+    fetch(0, s_codes0);
+    fetch_scales(0, s_scales[0]);
+    auto block = [&](uint32_t kb, int in4, const uint8_t* here, uint8_t* free) __attribute__((always_inline)) {
+        // what this wave fetched is in LDS (a barrier alone does not wait for loads into LDS), and behind the barrier what all did;
+        // the other buffer has been read
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        if (in4 == 0) {
+            const uint32_t* from = reinterpret_cast<const uint32_t*>(s_scales[kb / 4 % 2]);
 #pragma unroll
-            for (int i = 0; i < TM; ++i) scale_a[i] = s_scales[(kb / 4) % 2][wm + i * 16 + in16];
+            for (int i = 0; i < TM; ++i) sa[i] = from[wm + i * 16 + in16];
 #pragma unroll
-            for (int j = 0; j < TN; ++j) scale_b[j] = s_scales[(kb / 4) % 2][BM + wn + j * 16 + in16];
+            for (int j = 0; j < TN; ++j) sb[j] = from[BM + wn + j * 16 + in16];
         }
         intx8 va[TM], vb[TN];
 #pragma unroll
-        for (int j = 0; j < TN; ++j) vb[j] = operand(buf, BM + wn + j * 16);
+        for (int j = 0; j < TN; ++j) vb[j] = operand(here, BM + wn + j * 16);
 #pragma unroll
-        for (int i = 0; i < TM; ++i) va[i] = operand(buf, wm + i * 16);
-        if (kb + 1 < nb) {
-            fetch(kb + 1, buf ^ 1);
-            if (kb % 4 == 3) fetch_scales(kb + 1, ((kb + 1) / 4) % 2);
-        }
-        // B is the instruction's first operand: a lane then holds four consecutive columns of C
-        if constexpr (kExact) {
-            float fa[TM], fb[TN];
+        for (int i = 0; i < TM; ++i) va[i] = operand(here, wm + i * 16);
+        __builtin_amdgcn_sched_barrier(0);         // the loads behind the reads that the first products wait for
+        fetch(kb + 1 < nb ? kb + 1 : nb - 1, free);
+        if (in4 == 3) fetch_scales(kb + 1 < nb ? kb + 1 : kb & ~3u, s_scales[(kb + 1) / 4 % 2]);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int i = 0; i < TM; ++i) fa[i] = scale_value(scale_a[i] & 255u);
+        for (int i = 0; i < TM; ++i)
 #pragma unroll
-            for (int j = 0; j < TN; ++j) fb[j] = scale_value(scale_b[j] & 255u);
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                bf16x8 xa[TM], xb[TN];
-#pragma unroll
-                for (int j = 0; j < TN; ++j) xb[j] = decode_bf16(vb[j][2 * q], vb[j][2 * q + 1], fb[j]);
-#pragma unroll
-                for (int i = 0; i < TM; ++i) xa[i] = decode_bf16(va[i][2 * q], va[i][2 * q + 1], fa[i]);
-#pragma unroll
-                for (int i = 0; i < TM; ++i)
-#pragma unroll
-                    for (int j = 0; j < TN; ++j) sum[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xb[j], xa[i], sum[i][j], 0, 0, 0);
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < TM; ++i)
-#pragma unroll
-                for (int j = 0; j < TN; ++j)
-                    sum[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(vb[j], va[i], sum[i][j], 0, 0, 0, (int)scale_b[j], 0, (int)scale_a[i]);
-        }
-#pragma unroll
-        for (int i = 0; i < TM; ++i) scale_a[i] >>= 8;
-#pragma unroll
-        for (int j = 0; j < TN; ++j) scale_b[j] >>= 8;
+            for (int j = 0; j < TN; ++j) sum[i][j] = multiply<EXACT>(vb[j], sb[j] >> (8 * in4), va[i], sa[i] >> (8 * in4), sum[i][j]);
+    };
+    for (uint32_t kb = 0; kb < nb; kb += 4) {
+        block(kb, 0, s_codes0, s_codes1);
+        if (kb + 1 < nb) block(kb + 1, 1, s_codes1, s_codes0);
+        if (kb + 2 < nb) block(kb + 2, 2, s_codes0, s_codes1);
+        if (kb + 3 < nb) block(kb + 3, 3, s_codes1, s_codes0);
     }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // the last loads into LDS, which nobody reads, end before the block does
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
         const int64_t m = m0 + wm + i * 16 + in16;
@@ -239,7 +236,7 @@ __global__ __launch_bounds__(kThinWaves * kWave) void k_product_thin(PackedMatri
         for (int u = 0; u < kAhead; ++u) {
             if (k0 + u * kThinWaves < nb) {
 #pragma unroll
-                for (int i = 0; i < TM; ++i) sum[i] = multiply<D>(vb[u], sb[u], va[u][i], sa[u][i], sum[i]);
+                for (int i = 0; i < TM; ++i) sum[i] = multiply<Exact<D>::value>(vb[u], sb[u], va[u][i], sa[u][i], sum[i]);
             }
         }
     }
