@@ -53,27 +53,41 @@ PackGrid pack_grid(int64_t rows, int64_t cols, dim3* grid) {
     return g;
 }
 
-// How the weight gradient's sums are cut: tiles of 128 x 128 of every worker, and where they are too few for the
-// chip's 256 compute units (two blocks each), shares of the rows, at least kGradShareRows long, summed from the workspace.
+// How the weight gradient's sums are cut: tiles of every worker's gradient, and where they are too few for the chip's 256 compute
+// units, shares of the rows, joined from the workspace.
 struct GradPlan {
+    bool big;                           // tiles of 256 x 256, one block per compute unit; else 128 x 128 and two
     uint32_t tiles_n, tiles_k, splits;
     int64_t part_stride;                // values of one worker's share
     uint64_t jobs;
 };
-constexpr uint64_t kGradBlocks = 512;
-constexpr int64_t kGradShareRows = 256;
 constexpr uint64_t kMaxJobs = 0x7FFFFFFF;
-GradPlan grad_plan(int64_t rows, int32_t P, int64_t N, int64_t K) {
+constexpr int64_t kGradShareRows = 256, kGradShareRowsBig = 512;    // rows of a share, at least
+constexpr uint32_t kGradBand = 4, kGradBandBig = 8;                 // tiles across in a band (tile_at)
+GradPlan grad_plan_of(bool big, int64_t rows, int32_t P, int64_t N, int64_t K) {
     GradPlan g;
-    g.tiles_n = (uint32_t)ceil_div(N, 128);
-    g.tiles_k = (uint32_t)ceil_div(K, 128);
+    const int64_t side = big ? 256 : 128;
+    g.big = big;
+    g.tiles_n = (uint32_t)ceil_div(N, side);
+    g.tiles_k = (uint32_t)ceil_div(K, side);
     const uint64_t blocks = (uint64_t)g.tiles_n * g.tiles_k * (uint64_t)P;
-    const int64_t most = rows / P / kGradShareRows, want = (int64_t)(kGradBlocks / blocks);
+    const int64_t most = rows / P / (big ? kGradShareRowsBig : kGradShareRows), want = (int64_t)((big ? 256 : 512) / blocks);
     g.splits = (uint32_t)(want < most ? want : most);
     if (g.splits < 1) g.splits = 1;
     g.part_stride = ceil_div(N * K, 4) * 4;
     g.jobs = blocks * g.splits;
     return g;
+}
+// Large tiles for sums of at least kGradShareRowsBig rows in bf16 (an fp16 or fp32 dY's two or three parts do not fit the
+// registers beside their sums), if they keep three quarters of the chip at work and add at most a quarter to
+// what the small ones compute behind the edges.  (In us, small / large: 16384 rows, 1024 x 1024 59 / 55; 4096 x 4096 677 / 463;
+// 64 rows of 16 workers, 4096 x 9216: 438 / 533.)
+GradPlan grad_plan(bool bf16, int64_t rows, int32_t P, int64_t N, int64_t K) {
+    const GradPlan small = grad_plan_of(false, rows, P, N, K);
+    if (!bf16 || rows / P < kGradShareRowsBig) return small;
+    const GradPlan large = grad_plan_of(true, rows, P, N, K);
+    const bool fits = 4 * 4 * (uint64_t)large.tiles_n * large.tiles_k <= 5 * (uint64_t)small.tiles_n * small.tiles_k;
+    return fits && large.jobs >= 192 ? large : small;
 }
 
 }  // namespace
@@ -199,9 +213,14 @@ int gtopk_scaled_product(const uint8_t* a_codes, int64_t a_code_stride, const ui
 
 size_t gtopk_weight_grad_workspace_bytes(int64_t rows, int32_t P, int64_t N, int64_t K) {
     if (!side_ok(rows, 0) || P < 1 || P > 32768 || !side_ok(N, 1) || !side_ok(K, 1)) return 0;
-    const GradPlan g = grad_plan(rows, P, N, K);
-    if (g.jobs > kMaxJobs) return 0;
-    return 256 + (g.splits > 1 ? (size_t)g.splits * P * g.part_stride * sizeof(float) : 0);
+    size_t most = 0;                    // of the plans of all types
+    for (int bf16 = 0; bf16 < 2; ++bf16) {
+        const GradPlan g = grad_plan(bf16 != 0, rows, P, N, K);
+        if (g.jobs > kMaxJobs) return 0;
+        const size_t bytes = 256 + (g.splits > 1 ? (size_t)g.splits * P * g.part_stride * sizeof(float) : 0);
+        if (bytes > most) most = bytes;
+    }
+    return most;
 }
 
 int gtopk_weight_grad(const void* dy, int32_t dtype, int64_t dy_stride, const uint8_t* codes, int64_t code_stride,
@@ -214,15 +233,26 @@ int gtopk_weight_grad(const void* dy, int32_t dtype, int64_t dy_stride, const ui
     if (!aligned(dy, value_bytes(dtype)) || !packed_aligned(codes, scales) || !aligned(row_begin, 4) || !aligned(grad, 4) || !aligned(ws, 16))
         return GTOPK_EALIGN;
     if (ws_bytes < need) return GTOPK_EWORKSPACE;
-    const GradPlan g = grad_plan(rows, P, N, K);
+    const GradPlan g = grad_plan(dtype == GTOPK_BF16, rows, P, N, K);
     const bool split = g.splits > 1;
+    float* const to = split ? (float*)ws : grad;
+    const int64_t to_stride = split ? g.part_stride : grad_stride, split_stride = split ? g.part_stride * P : 0;
+    // Where a row's tiles end inside memory lines, whole rows of tiles run side by side, so that the two writes of a line meet
+    // in L2 (4096 x 9217: 3.4 TB/s in bands of 4 tiles, 5.0 in whole rows); otherwise bands are the better (4096 x 4096: 5.5 and 4.8)
+    const bool whole_lines = K % 32 == 0 && to_stride % 32 == 0 && aligned(to, 128);
+    const uint32_t band = !whole_lines ? g.tiles_k : g.big ? kGradBandBig : kGradBand;
     hipStream_t st = (hipStream_t)stream;
     by_type(dtype, [&](auto d) {
         using D = decltype(d);
-        hipLaunchKernelGGL((k_weight_grad<D, 128, 128, 64, 64>), dim3(grid_for(g.jobs)), dim3(256), 0, st, (const typename D::T*)dy,
-                           dy_stride, codes, code_stride, scales, scale_stride, rows, row_begin, (uint32_t)P, N, K,
-                           split ? (float*)ws : grad, split ? g.part_stride : grad_stride, split ? 0 : accumulate != 0, g.splits,
-                           split ? g.part_stride * P : 0, g.tiles_n, g.tiles_k, (uint32_t)g.jobs);
+        auto launch = [&](auto kernel, int threads) {
+            hipLaunchKernelGGL(kernel, dim3(grid_for(g.jobs)), dim3(threads), 0, st, (const typename D::T*)dy, dy_stride, codes, code_stride,
+                               scales, scale_stride, rows, row_begin, (uint32_t)P, N, K, to, to_stride, split ? 0 : accumulate != 0,
+                               g.splits, split_stride, g.tiles_n, g.tiles_k, band, (uint32_t)g.jobs);
+        };
+        if constexpr (Parts<D>::n == 1) {
+            if (g.big) return launch(k_weight_grad<D, 256, 256, 128, 64>, 512);
+        }
+        launch(k_weight_grad<D, 128, 128, 64, 64>, 256);
     });
     if (split) {
         const int64_t blocks = ceil_div(N * K, 4 * kPackThreads);

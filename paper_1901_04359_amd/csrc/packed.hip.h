@@ -27,13 +27,17 @@ struct F32 { typedef float T; };
 struct BF16 { typedef __bf16 T; };
 struct F16 { typedef _Float16 T; };
 
+template <class D> using Eight = typename D::T __attribute__((ext_vector_type(kLaneVals)));
+
 // 8 consecutive values; p is aligned to one value (global memory takes wide accesses at any address)
 template <class D>
+__device__ __forceinline__ Eight<D> load_eight(const typename D::T* p) {
+    struct __attribute__((packed)) Loose { Eight<D> v; };
+    return reinterpret_cast<const Loose*>(p)->v;
+}
+template <class D>
 __device__ __forceinline__ void load8(const typename D::T* p, float (&v)[kLaneVals]) {
-    typedef typename D::T T;
-    typedef T Vec __attribute__((ext_vector_type(kLaneVals)));
-    struct __attribute__((packed)) Loose { Vec v; };
-    const Vec x = reinterpret_cast<const Loose*>(p)->v;
+    const Eight<D> x = load_eight<D>(p);
 #pragma unroll
     for (int j = 0; j < kLaneVals; ++j) v[j] = (float)x[j];
 }
@@ -146,6 +150,21 @@ template <bool UPPER>
 __device__ __forceinline__ uint32_t decode2(uint32_t c, float scale) {
     const bf16x2 v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, scale, UPPER);
     return __builtin_bit_cast(uint32_t, v);
+}
+
+// Number `id` of `count` so that the ids that one XCD gets (id % 8, blocks are dealt out in turn) are consecutive numbers
+__device__ __forceinline__ uint32_t by_xcd(uint32_t id, uint32_t count) {
+    const uint32_t xcd = id % 8, each = count / 8, more = count % 8;
+    return xcd * each + (xcd < more ? xcd : more) + id / 8;
+}
+
+// tile `t` of tiles_m x tiles_n: columns of `high` tiles, one column of tiles after the other, so that the tiles that are
+// worked on side by side are about as many down as across and share their rows of A and B in an XCD's L2
+__device__ __forceinline__ void tile_at(uint32_t t, uint32_t tiles_m, uint32_t tiles_n, uint32_t high, uint32_t& m, uint32_t& n) {
+    const uint32_t band = t / (high * tiles_n), first = band * high, in = t - band * high * tiles_n;
+    const uint32_t rows = tiles_m - first < high ? tiles_m - first : high;
+    m = first + in % rows;
+    n = in / rows;
 }
 
 // How the 16 blocks of 128 that a thread block covers lie in the matrix: 2^side_log2 of them side by side, the rest below

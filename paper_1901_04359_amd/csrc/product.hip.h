@@ -59,21 +59,6 @@ __device__ __forceinline__ floatx4 multiply(intx8 vb, uint32_t sb, intx8 va, uin
     }
 }
 
-// Number `id` of `count` so that the ids that one XCD gets (id % 8, blocks are dealt out in turn) are consecutive numbers
-__device__ __forceinline__ uint32_t by_xcd(uint32_t id, uint32_t count) {
-    const uint32_t xcd = id % 8, each = count / 8, more = count % 8;
-    return xcd * each + (xcd < more ? xcd : more) + id / 8;
-}
-
-// tile `t` of tiles_m x tiles_n: columns of `high` tiles, one column of tiles after the other, so that the tiles that are
-// worked on side by side are about as many down as across and share their rows of A and B in an XCD's L2
-__device__ __forceinline__ void tile_at(uint32_t t, uint32_t tiles_m, uint32_t tiles_n, uint32_t high, uint32_t& m, uint32_t& n) {
-    const uint32_t band = t / (high * tiles_n), first = band * high, in = t - band * high * tiles_n;
-    const uint32_t rows = tiles_m - first < high ? tiles_m - first : high;
-    m = first + in % rows;
-    n = in / rows;
-}
-
 // A block computes BM x BN values with BM/WM x BN/WN waves of WM x WN each.  A block of 128 of the tile's rows of A and B
 // goes straight from global memory into one of two LDS buffers while the matrix instructions work on the other; the scales
 // of four blocks go together (a word per row: fetched one by one they would be as many requests as the codes).

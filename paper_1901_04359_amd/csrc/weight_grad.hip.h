@@ -33,20 +33,27 @@ template <> struct Parts<BF16> { static constexpr int n = 1; };
 template <> struct Parts<F16> { static constexpr int n = 2; };
 template <> struct Parts<F32> { static constexpr int n = 3; };
 
-// bits of the parts of two values, packed: part[i] = low half from a, high half from b
-template <int N>
-__device__ __forceinline__ void split2(float a, float b, uint32_t (&part)[N]) {
-    auto lead = [](float v) {
-        const uint32_t u = __float_as_uint(v);
-        return v != v ? u | 0x00400000u : u;        // NaN: the bit that is kept must not be 0
-    };
-    const bool fa = finite_bits(__float_as_uint(a)), fb = finite_bits(__float_as_uint(b));
+// the parts of 8 values, 8 numbers of 16 bits each
+__device__ __forceinline__ void parts_of(Eight<BF16> v, uint32x4 (&part)[1]) { part[0] = __builtin_bit_cast(uint32x4, v); }
+template <class T, int N>
+__device__ __forceinline__ void parts_of(T v, uint32x4 (&part)[N]) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const uint32_t ua = lead(a), ub = lead(b);
-        part[i] = __builtin_amdgcn_perm(ub, ua, 0x07060302u);
-        a = fa ? a - __uint_as_float(ua & 0xFFFF0000u) : 0.0f;
-        b = fb ? b - __uint_as_float(ub & 0xFFFF0000u) : 0.0f;
+    for (int j = 0; j < 4; ++j) {
+        // (a signalling NaN, whose upper half may be that of an infinity, becomes a quiet one)
+        float a = __builtin_canonicalizef((float)v[2 * j]), b = __builtin_canonicalizef((float)v[2 * j + 1]);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const uint32_t ua = __float_as_uint(a), ub = __float_as_uint(b);
+            part[i][j] = __builtin_amdgcn_perm(ub, ua, 0x07060302u);
+            if (i + 1 < N) {
+                a -= __uint_as_float(ua & 0xFFFF0000u);
+                b -= __uint_as_float(ub & 0xFFFF0000u);
+                if (i == 0) {              // behind an infinity nothing is left
+                    a = finite_bits(ua) ? a : 0.0f;
+                    b = finite_bits(ub) ? b : 0.0f;
+                }
+            }
+        }
     }
 }
 
@@ -61,22 +68,26 @@ __device__ __forceinline__ void decode16(uint32x4 c, float scale, uint32x4& lo, 
     }
 }
 
-// What a block loads ahead: kRows rows of the tile's columns of dY and X.
-constexpr int kGradRows = 32;
+constexpr int kGradRows = 32;               // rows of dY and X in one step
 
 // A block computes BN x BK values of one worker (rows of dW from dY's columns, columns from X's) over all of its rows,
 // or over one of `splits` equal shares of them, with waves of WN x WK.  kGradRows rows at a time lie in one of two LDS
-// buffers while the next ones are on their way to registers.  In LDS both are bf16 with their rows as in
+// buffers; the rows of the next two steps are on their way to registers.  In LDS both matrices are bf16 with their rows as in
 // memory; ds_read_b64_tr_b16 gives each lane four rows' values of one column, which is what the
 // matrix instruction wants.  (Which 8 of the 32 rows a lane holds is free as long as both operands agree: the
 // four groups of 16 lanes take rows 4 g .. 4 g + 3 and 16 + 4 g .. , so that with 8 words between the rows'
 // banks 16 lanes' pieces of 32 bytes fall on all of them.)
+// Tiles of 128 x 128 with four waves, two blocks per compute unit: where workers have few rows, writing dW bounds the call (16
+// workers, 64 rows each, 4096 x 9216: 2.4 GB in 440 us = 5.6 TB/s).  Tiles of 256 x 256 with eight waves for long sums in
+// bf16: half the LDS traffic and loads per product (16384 rows, 4096 x 4096: 463 us = 1.19 PFLOP/s, with tiles of 128 677 us);
+// there (kAhead) the next rows are staged while the matrix instructions run, also behind the last step, which would cost
+// a quarter of the call where workers have two steps.
 template <class D, int BN, int BK, int WN, int WK>
-__global__ __launch_bounds__((BN / WN) * (BK / WK) * kWave, 2) void k_weight_grad(
+__global__ __launch_bounds__((BN / WN) * (BK / WK) * kWave, BN * BK > 128 * 128 ? 1 : 2) void k_weight_grad(
         const typename D::T* __restrict__ dy, int64_t dy_stride, const uint8_t* __restrict__ codes, int64_t code_stride,
         const uint8_t* __restrict__ scales, int64_t scale_stride, int64_t rows, const int32_t* __restrict__ begin, uint32_t P,
         int64_t N, int64_t K, float* __restrict__ grad, int64_t grad_stride, int accumulate, uint32_t splits, int64_t split_stride,
-        uint32_t tiles_n, uint32_t tiles_k, uint32_t jobs) {
+        uint32_t tiles_n, uint32_t tiles_k, uint32_t band, uint32_t jobs) {
     constexpr int kParts = Parts<D>::n;
     constexpr int kWavesK = BK / WK, kThreads = (BN / WN) * kWavesK * kWave;
     constexpr int TN = WN / 16, TK = WK / 16;
@@ -84,17 +95,21 @@ __global__ __launch_bounds__((BN / WN) * (BK / WK) * kWave, 2) void k_weight_gra
     constexpr int kLoadsD = kGradRows * BN / 8 / kThreads, kLoadsX = kGradRows * BK / 16 / kThreads;
     static_assert(kLoadsD * kThreads * 8 == kGradRows * BN && kLoadsX * kThreads * 16 == kGradRows * BK, "whole loads");
     static_assert(BK % kPackBlock == 0, "a lane's 16 codes lie in one block of 128");
-    __shared__ __align__(16) uint16_t s_d[2][kParts][kGradRows * kPitchD];
-    __shared__ __align__(16) uint16_t s_x[2][kGradRows * kPitchX];
+    constexpr bool kAhead = BN * BK > 128 * 128;
+    constexpr int kPitchOut = WK + 4;                                      // floats
+    static_assert((BN / WN) * kWavesK * 16 * kPitchOut * 2 <= 2 * kGradRows * (kParts * kPitchD + kPitchX), "the result's rows fit the same memory");
+    __shared__ __align__(16) uint16_t s_rows[2 * kGradRows * (kParts * kPitchD + kPitchX)];
+    uint16_t* const s_d = s_rows;                                          // [2][kParts][kGradRows][kPitchD]
+    uint16_t* const s_x = s_rows + 2 * kParts * kGradRows * kPitchD;       // [2][kGradRows][kPitchX]
 
     const uint32_t wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
     const uint32_t wn = (wave / kWavesK) * WN, wk = (wave % kWavesK) * WK;
     for (uint32_t id = blockIdx.x; id < jobs; id += gridDim.x) {
-        uint32_t job = id;
-        const uint32_t tile_k = job % tiles_k;
-        job /= tiles_k;
-        const uint32_t tile_n = job % tiles_n;
-        job /= tiles_n;
+        uint32_t job = by_xcd(id, jobs);
+        const uint32_t tiles = tiles_n * tiles_k;
+        uint32_t tile_n, tile_k;
+        tile_at(job % tiles, tiles_k, tiles_n, band, tile_k, tile_n);
+        job /= tiles;
         const uint32_t split = job % splits, w = job / splits;
         const int64_t n0 = (int64_t)tile_n * BN, k0 = (int64_t)tile_k * BK;
         int64_t first, last;
@@ -114,50 +129,51 @@ __global__ __launch_bounds__((BN / WN) * (BK / WK) * kWave, 2) void k_weight_gra
         const typename D::T* d_from = dy + (first + d_row) * dy_stride + n0 + n_at;
         const uint8_t* x_from = codes + (first + x_row) * code_stride + k0 + k_at;
         const uint8_t* s_from = scales + (first + x_row) * scale_stride + (k0 + k_at) / kPackBlock;
-        float d_next[kLoadsD][kLaneVals];
-        uint32x4 x_next[kLoadsX];
-        uint32_t s_next[kLoadsX];
-        auto load = [&](int32_t step) {
-            const int64_t left = last - first - (int64_t)step * kGradRows;     // rows from this step on
+        int32_t left = (int32_t)(last - first);    // rows that have not been loaded
+        // two steps' rows on their way, as they lie in memory: taken apart when they are staged
+        Eight<D> d_next[2][kLoadsD];
+        uint32x4 x_next[2][kLoadsX];
+        uint32_t s_next[2][kLoadsX];
+        auto load = [&](int set) __attribute__((always_inline)) {      // the next step's rows
 #pragma unroll
             for (int i = 0; i < kLoadsD; ++i) {
-                const int r = d_row + i * (kThreads * 8 / BN);
-                const typename D::T* p = d_from + ((int64_t)step * kGradRows + i * (kThreads * 8 / BN)) * dy_stride;
-                if (r < left && n_left >= kLaneVals) load8<D>(p, d_next[i]);
-                else load_some<D>(p, r < left ? (int)n_left : 0, d_next[i]);
+                const bool in = (int)d_row + i * (kThreads * 8 / BN) < left;
+                const typename D::T* p = d_from + i * (kThreads * 8 / BN) * dy_stride;
+                if (in && n_left >= kLaneVals) {
+                    d_next[set][i] = load_eight<D>(p);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < kLaneVals; ++j) d_next[set][i][j] = in && j < n_left ? p[j] : (typename D::T)0.0f;
+                }
             }
 #pragma unroll
             for (int i = 0; i < kLoadsX; ++i) {
-                const int r = x_row + i * (kThreads * 16 / BK);
-                const int64_t at = (int64_t)step * kGradRows + i * (kThreads * 16 / BK);
-                x_next[i] = uint32x4{0u, 0u, 0u, 0u};
-                s_next[i] = 127u;
-                if (r < left && k_in) {
-                    x_next[i] = *reinterpret_cast<const uint32x4*>(x_from + at * code_stride);
-                    s_next[i] = s_from[at * scale_stride];
+                x_next[set][i] = uint32x4{0u, 0u, 0u, 0u};
+                s_next[set][i] = 127u;
+                if ((int)x_row + i * (kThreads * 16 / BK) < left && k_in) {
+                    x_next[set][i] = *reinterpret_cast<const uint32x4*>(x_from + i * (kThreads * 16 / BK) * code_stride);
+                    s_next[set][i] = s_from[i * (kThreads * 16 / BK) * scale_stride];
                 }
             }
+            d_from += kGradRows * dy_stride;
+            x_from += kGradRows * code_stride;
+            s_from += kGradRows * scale_stride;
+            left -= kGradRows;
         };
-        auto stage = [&](int buf) {
+        auto stage = [&](int buf, int set) __attribute__((always_inline)) {
 #pragma unroll
             for (int i = 0; i < kLoadsD; ++i) {
                 uint32x4 word[kParts];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    uint32_t part[kParts];
-                    split2(d_next[i][2 * j], d_next[i][2 * j + 1], part);
-#pragma unroll
-                    for (int q = 0; q < kParts; ++q) word[q][j] = part[q];
-                }
+                parts_of(d_next[set][i], word);
 #pragma unroll
                 for (int q = 0; q < kParts; ++q)
-                    *reinterpret_cast<uint32x4*>(s_d[buf][q] + (d_row + i * (kThreads * 8 / BN)) * kPitchD + n_at) = word[q];
+                    *reinterpret_cast<uint32x4*>(s_d + ((buf * kParts + q) * kGradRows + d_row + i * (kThreads * 8 / BN)) * kPitchD + n_at) = word[q];
             }
 #pragma unroll
             for (int i = 0; i < kLoadsX; ++i) {
                 uint32x4 lo, hi;
-                decode16(x_next[i], scale_value(s_next[i]), lo, hi);
-                uint32x4* to = reinterpret_cast<uint32x4*>(s_x[buf] + (x_row + i * (kThreads * 16 / BK)) * kPitchX + k_at);
+                decode16(x_next[set][i], scale_value(s_next[set][i]), lo, hi);
+                uint32x4* to = reinterpret_cast<uint32x4*>(s_x + (buf * kGradRows + x_row + i * (kThreads * 16 / BK)) * kPitchX + k_at);
                 to[0] = lo;
                 to[1] = hi;
             }
@@ -171,50 +187,73 @@ __global__ __launch_bounds__((BN / WN) * (BK / WK) * kWave, 2) void k_weight_gra
         };
 
         floatx4 sum[TK][TN] = {};
-        if (steps > 0) {
-            load(0);
-            stage(0);
-            __syncthreads();
-        }
-        for (int32_t step = 0; step < steps; ++step) {
-            const int buf = step % 2;
-            if (step + 1 < steps) load(step + 1);
+        auto step_at = [&](int32_t step, int buf) __attribute__((always_inline)) {
             bf16x8 x[TK];
 #pragma unroll
-            for (int i = 0; i < TK; ++i) x[i] = operand(s_x[buf], kPitchX, wk + i * 16);
+            for (int i = 0; i < TK; ++i) x[i] = operand(s_x + buf * kGradRows * kPitchX, kPitchX, wk + i * 16);
+            if constexpr (kAhead) {
+                stage(buf ^ 1, buf ^ 1);
+                load(buf ^ 1);
+            }
 #pragma unroll
             for (int q = 0; q < kParts; ++q) {
                 bf16x8 d[TN];
 #pragma unroll
-                for (int j = 0; j < TN; ++j) d[j] = operand(s_d[buf][q], kPitchD, wn + j * 16);
+                for (int j = 0; j < TN; ++j) d[j] = operand(s_d + (buf * kParts + q) * kGradRows * kPitchD, kPitchD, wn + j * 16);
 #pragma unroll
                 for (int i = 0; i < TK; ++i)
 #pragma unroll
                     for (int j = 0; j < TN; ++j) sum[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[i], d[j], sum[i][j], 0, 0, 0);
             }
-            if (step + 1 < steps) stage(buf ^ 1);
+            if constexpr (!kAhead) {
+                if (step + 1 < steps) {
+                    stage(buf ^ 1, buf ^ 1);
+                    load(buf ^ 1);         // (rows behind the last one are not read)
+                }
+            }
+            __syncthreads();
+        };
+        if (steps > 0) {
+            load(0);
+            load(1);
+            stage(0, 0);
+            load(0);
             __syncthreads();
         }
-        // a lane holds four consecutive columns of a row of dW
+        int32_t step = 0;
+        for (; step + 2 <= steps; step += 2) {
+            step_at(step, 0);
+            step_at(step + 1, 1);
+        }
+        if (step < steps) step_at(step, 0);
+        // A lane holds four consecutive columns of a row of dW, and a wave's store would write pieces of 64 bytes of 16 rows; by way
+        // of LDS (each wave its own part, 16 rows at a time) it writes 4 WK bytes of a row at a stretch.
         float* const to = grad + w * grad_stride + split * split_stride;
+        float* const s_out = reinterpret_cast<float*>(s_rows) + wave * 16 * kPitchOut;
+        constexpr int kAcross = WK / 4;        // lanes per row
 #pragma unroll
         for (int j = 0; j < TN; ++j) {
-            const int64_t n = n0 + wn + j * 16 + lane % 16;
-            if (n >= N) continue;
 #pragma unroll
-            for (int i = 0; i < TK; ++i) {
-                const int64_t k = k0 + wk + i * 16 + lane / 16 * 4;
-                if (k >= K) continue;
-                float* p = to + n * K + k;
-                floatx4 v = sum[i][j];
-                if (accumulate) {
+            for (int i = 0; i < TK; ++i) *reinterpret_cast<floatx4*>(s_out + lane % 16 * kPitchOut + i * 16 + lane / 16 * 4) = sum[i][j];
+            __builtin_amdgcn_wave_barrier();
 #pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        if (k + r < K) v[r] = p[r] + v[r];
+            for (int r = 0; r < 16; r += kWave / kAcross) {
+                const int row = r + lane / kAcross, col = lane % kAcross * 4;
+                floatx4 v = *reinterpret_cast<const floatx4*>(s_out + row * kPitchOut + col);
+                const int64_t n = n0 + wn + j * 16 + row, k = k0 + wk + col;
+                if (n < N && k < K) {
+                    float* p = to + n * K + k;
+                    if (accumulate) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (k + e < K) v[e] = p[e] + v[e];
+                    }
+                    store4<F32>(p, K - k, v);
                 }
-                store4<F32>(p, K - k, v);
             }
+            __builtin_amdgcn_wave_barrier();
         }
+        if (id + gridDim.x < jobs) __syncthreads();        // the next job's rows go where the result's were
     }
 }
 

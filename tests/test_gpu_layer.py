@@ -343,7 +343,8 @@ def begins(P, rows, kind, seed=0):
 GRADS = [(1, 1, 1, 1, "even"), (1, 1, 5, 300, "even"), (4, 4, 3, 2, "even"), (2, 64, 16, 16, "even"), (8, 8, 130, 129, "even"),
          (3, 33, 17, 40, "ragged"), (4, 100, 64, 128, "loose"), (2, 500, 128, 128, "even"), (1, 2000, 100, 260, "even"),
          (5, 77, 257, 385, "ragged"), (1, 9000, 33, 65, "even"), (8, 1501, 100, 131, "ragged"), (16, 1024, 256, 130, "even"),
-         (1, 0, 20, 30, "even"), (6, 3, 9, 140, "loose"), (32, 32 * 40, 40, 200, "even")]
+         (1, 0, 20, 30, "even"), (6, 3, 9, 140, "loose"), (32, 32 * 40, 40, 200, "even"),
+         (2, 6000, 1000, 1100, "ragged"), (3, 4700, 1025, 770, "loose"), (1, 9001, 1030, 900, "even")]
 
 
 @pytest.mark.parametrize("P,rows,N,K,kind", GRADS)
