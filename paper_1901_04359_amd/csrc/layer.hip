@@ -4,6 +4,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "gtopk.h"
 #include "common.hip.h"
 #include "packed.hip.h"
@@ -41,14 +43,27 @@ void by_type(int32_t dtype, L launch) {
     else launch(F16{});
 }
 
-PackGrid pack_grid(int64_t rows, int64_t cols, dim3* grid) {
+// calls launch(std::integral_constant<int, act>{})
+template <class L>
+void by_act(int32_t act, L launch) {
+    switch (act) {
+        case GTOPK_ACT_RELU: return launch(std::integral_constant<int, GTOPK_ACT_RELU>{});
+        case GTOPK_ACT_TANH: return launch(std::integral_constant<int, GTOPK_ACT_TANH>{});
+        case GTOPK_ACT_SIGMOID: return launch(std::integral_constant<int, GTOPK_ACT_SIGMOID>{});
+        case GTOPK_ACT_SILU: return launch(std::integral_constant<int, GTOPK_ACT_SILU>{});
+        case GTOPK_ACT_GELU: return launch(std::integral_constant<int, GTOPK_ACT_GELU>{});
+        default: return launch(std::integral_constant<int, GTOPK_ACT_NONE>{});
+    }
+}
+
+PackGrid pack_grid(int64_t rows, int64_t cols, int32_t dtype, dim3* grid) {
     PackGrid g;
     g.rows = rows;
     g.cols = cols;
     g.nb = (uint32_t)ceil_div(cols, kPackBlock);
     g.side_log2 = 0;
     while (g.side_log2 < 4 && (1u << g.side_log2) < g.nb) ++g.side_log2;
-    const int64_t deep = (kPackThreads / 16) >> g.side_log2, down = ceil_div(rows, deep);
+    const int64_t deep = ((kPackThreads / 16) >> g.side_log2) * rows_ahead(value_bytes(dtype)), down = ceil_div(rows, deep);
     *grid = dim3((uint32_t)ceil_div(g.nb, 1 << g.side_log2), (uint32_t)(down < 65535 ? down : 65535));
     return g;
 }
@@ -102,7 +117,7 @@ int gtopk_pack_rows(const void* x, int32_t dtype, int64_t rows, int64_t cols, in
     if (!x || !codes || !scales) return GTOPK_EINVAL;
     if (!aligned(x, value_bytes(dtype)) || !packed_aligned(codes, scales)) return GTOPK_EALIGN;
     dim3 grid;
-    const PackGrid g = pack_grid(rows, cols, &grid);
+    const PackGrid g = pack_grid(rows, cols, dtype, &grid);
     by_type(dtype, [&](auto d) {
         using D = decltype(d);
         hipLaunchKernelGGL(k_pack_rows<D>, grid, dim3(kPackThreads), 0, (hipStream_t)stream, (const typename D::T*)x, stride, g,
@@ -140,11 +155,13 @@ int gtopk_unpack(const uint8_t* codes, int64_t code_stride, const uint8_t* scale
     if (!codes || !scales || !out) return GTOPK_EINVAL;
     if (!packed_aligned(codes, scales) || !aligned(out, value_bytes(dtype))) return GTOPK_EALIGN;
     dim3 grid;
-    const PackGrid g = pack_grid(rows, cols, &grid);
+    const PackGrid g = pack_grid(rows, cols, dtype, &grid);
     by_type(dtype, [&](auto d) {
         using D = decltype(d);
-        hipLaunchKernelGGL(k_unpack<D>, grid, dim3(kPackThreads), 0, (hipStream_t)stream, codes, code_stride, scales,
-                           scale_stride, g, (int)act, (typename D::T*)out, out_stride);
+        by_act(act, [&](auto f) {
+            hipLaunchKernelGGL((k_unpack<D, decltype(f)::value>), grid, dim3(kPackThreads), 0, (hipStream_t)stream, codes,
+                               code_stride, scales, scale_stride, g, (typename D::T*)out, out_stride);
+        });
     });
     return launch_status();
 }
@@ -159,11 +176,13 @@ int gtopk_activation_grad(const uint8_t* codes, int64_t code_stride, const uint8
     if (!codes || !scales || !dy || !dx || (dy == dx && dy_stride != dx_stride)) return GTOPK_EINVAL;
     if (!packed_aligned(codes, scales) || !aligned(dy, value_bytes(dtype)) || !aligned(dx, value_bytes(dtype))) return GTOPK_EALIGN;
     dim3 grid;
-    const PackGrid g = pack_grid(rows, cols, &grid);
+    const PackGrid g = pack_grid(rows, cols, dtype, &grid);
     by_type(dtype, [&](auto d) {
         using D = decltype(d);
-        hipLaunchKernelGGL(k_activation_grad<D>, grid, dim3(kPackThreads), 0, (hipStream_t)stream, codes, code_stride, scales,
-                           scale_stride, g, (int)act, (const typename D::T*)dy, dy_stride, (typename D::T*)dx, dx_stride);
+        by_act(act, [&](auto f) {
+            hipLaunchKernelGGL((k_activation_grad<D, decltype(f)::value>), grid, dim3(kPackThreads), 0, (hipStream_t)stream, codes,
+                               code_stride, scales, scale_stride, g, (const typename D::T*)dy, dy_stride, (typename D::T*)dx, dx_stride);
+        });
     });
     return launch_status();
 }

@@ -173,92 +173,169 @@ struct PackGrid {
     uint32_t nb;                            // blocks of 128 per row
     uint32_t side_log2;
 };
-// f(row, block of the row, lane's first column) for every block of 128, 16 lanes per block, all lanes of a row together
-template <class F>
-__device__ __forceinline__ void for_blocks(const PackGrid& g, F f) {
+// Rows whose loads a thread has under way before the first one's work: with 16 bytes per row and lane two are the better (unpack of
+// 8192 x 4096 to bf16: 17.5 us with one, 16.2 with two, 16.5 with four), with 32 bytes one is (to fp32: 25.9, 28.7, 28.1).
+constexpr int rows_ahead(size_t value_bytes) { return value_bytes == 4 ? 1 : 2; }
+// load(u, row, block of the row, lane's first column), then work(..) of the same, for every block of 128, 16 lanes per block, all
+// lanes of a block together
+template <int ROWS, class L, class W>
+__device__ __forceinline__ void for_blocks(const PackGrid& g, L load, W work) {
     const uint32_t item = threadIdx.x / 16, lane = threadIdx.x % 16;
     const uint32_t kb = (blockIdx.x << g.side_log2) + (item & ((1u << g.side_log2) - 1u));
-    const uint32_t deep = (kPackThreads / 16) >> g.side_log2;      // rows per thread block
+    const uint32_t deep = (kPackThreads / 16) >> g.side_log2;      // rows per thread block and turn
     if (kb >= g.nb) return;
-    for (int64_t row = (int64_t)blockIdx.y * deep + (item >> g.side_log2); row < g.rows; row += (int64_t)gridDim.y * deep)
-        f(row, kb, (int64_t)kb * kPackBlock + lane * kLaneVals);
+    const int64_t col = (int64_t)kb * kPackBlock + lane * kLaneVals;
+    for (int64_t row = (int64_t)blockIdx.y * deep * ROWS + (item >> g.side_log2); row < g.rows; row += (int64_t)gridDim.y * deep * ROWS) {
+#pragma unroll
+        for (int u = 0; u < ROWS; ++u)
+            if (row + u * deep < g.rows) load(u, row + u * deep, kb, col);
+#pragma unroll
+        for (int u = 0; u < ROWS; ++u)
+            if (row + u * deep < g.rows) work(u, row + u * deep, kb, col);
+    }
+}
+// the lane's values of a row of a dense matrix, 0 behind its end
+template <class D>
+__device__ __forceinline__ Eight<D> load_row(const typename D::T* p, int64_t left) {
+    Eight<D> v;
+    if (left >= kLaneVals) {
+        v = load_eight<D>(p);
+    } else {
+#pragma unroll
+        for (int j = 0; j < kLaneVals; ++j) v[j] = j < left ? p[j] : (typename D::T)0.0f;
+    }
+    return v;
+}
+template <class D>
+__device__ __forceinline__ void store_row(typename D::T* p, int64_t left, const float (&v)[kLaneVals]) {
+    if (left >= kLaneVals) store8<D>(p, v);
+    else store_some<D>(p, (int)left, v);
 }
 
 template <class D>
 __global__ __launch_bounds__(kPackThreads) void k_pack_rows(
         const typename D::T* __restrict__ x, int64_t stride, PackGrid g, uint8_t* __restrict__ codes, int64_t code_stride,
         uint8_t* __restrict__ scales, int64_t scale_stride) {
-    for_blocks(g, [&](int64_t row, uint32_t kb, int64_t col) {
+    constexpr int kRows = rows_ahead(sizeof(typename D::T));
+    Eight<D> in[kRows];
+    for_blocks<kRows>(g, [&](int u, int64_t row, uint32_t, int64_t col) { in[u] = load_row<D>(x + row * stride + col, g.cols - col); },
+               [&](int u, int64_t row, uint32_t kb, int64_t col) {
         float v[kLaneVals];
-        const int64_t left = g.cols - col;
-        const typename D::T* p = x + row * stride + col;
-        if (left >= kLaneVals) load8<D>(p, v);
-        else load_some<D>(p, (int)left, v);
+#pragma unroll
+        for (int j = 0; j < kLaneVals; ++j) v[j] = (float)in[u][j];
         const uint32_t s = scale_for(row_largest(top_of(v)));
         *reinterpret_cast<uint32x2*>(codes + row * code_stride + col) = encode8(v, inverse_scale(s));
         if (threadIdx.x % 16 == 0) scales[row * scale_stride + kb] = (uint8_t)s;
     });
 }
 
-// f and f' of the layer's activation, in 32 bits
-__device__ __forceinline__ float logistic(float x) { return 1.0f / (1.0f + expf(-x)); }
-__device__ __forceinline__ float act_value(int act, float x) {
-    switch (act) {
-        case GTOPK_ACT_RELU: return x < 0.0f ? 0.0f : x;              // NaN stays NaN
-        case GTOPK_ACT_TANH: return tanhf(x);
-        case GTOPK_ACT_SIGMOID: return logistic(x);
-        case GTOPK_ACT_SILU: return x * logistic(x);
-        case GTOPK_ACT_GELU: return x * 0.5f * erfcf(x * -0.70710678118654752f);
-        default: return x;
-    }
+// ---- f and f' of the layer's activation, in 32 bits -----------------------------------
+// Written for the rate of the memory: some twenty operations per value, each function from one exponential and one reciprocal.
+
+__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896341f); }   // off by 2^-23 max(1, |x|)
+__device__ __forceinline__ float reciprocal(float x) { return __builtin_amdgcn_rcpf(x); }                     // off by 2^-23
+// 1 / (1 + e^-x), without cancellation at either end
+__device__ __forceinline__ float logistic(float x) {
+    const float e = exp_of(-fabsf(x)), r = reciprocal(1.0f + e);
+    return x < 0.0f ? e * r : r;
 }
-__device__ __forceinline__ float act_slope(int act, float x) {
-    switch (act) {
-        case GTOPK_ACT_RELU: return x > 0.0f ? 1.0f : x <= 0.0f ? 0.0f : x;
-        case GTOPK_ACT_TANH: { const float t = tanhf(x); return (1.0f - t) * (1.0f + t); }
-        case GTOPK_ACT_SIGMOID: return logistic(x) * logistic(-x);
-        case GTOPK_ACT_SILU: { const float s = logistic(x); return s + x * (s * logistic(-x)); }
-        case GTOPK_ACT_GELU:
-            return 0.5f * erfcf(x * -0.70710678118654752f) + x * (0.39894228040143268f * expf(-0.5f * x * x));
-        default: return x == x ? 1.0f : x;
-    }
+// tanh x = (1 - e) / (1 + e) with e = exp(-2 |x|); below 1/4, where 1 - e cancels, the Taylor series to x^9 (the next term is 2^-26 there)
+__device__ __forceinline__ float tanh_of(float x) {
+    const float e = exp_of(-2.0f * fabsf(x)), far = copysignf((1.0f - e) * reciprocal(1.0f + e), x), s = x * x;
+    float p = fmaf(s, 62.0f / 2835.0f, -17.0f / 315.0f);
+    p = fmaf(s, p, 2.0f / 15.0f);
+    p = fmaf(s, p, -1.0f / 3.0f);
+    return fabsf(x) < 0.25f ? fmaf(x * s, p, x) : far;
+}
+// Phi(-|x|) = erfc(z) / 2 with z = |x| / sqrt 2, and e^(-x^2 / 2), as tail * bell.  For z >= 0, erfc(z) = e^(-z^2) t p(t) with
+// t = 1 / (1 + 0.3 z); p has degree 8, fitted to erfc(z) e^(z^2) / t for z up to 10.5 with weights that level the relative error:
+// 2^-25, evaluated in fp32 7e-7 up to z = 3.  (p is halved here.)
+__device__ __forceinline__ float normal_tail(float x, float& bell) {
+    const float t = reciprocal(fmaf(0.3f * 0.70710678118654752f, fabsf(x), 1.0f));
+    bell = __builtin_amdgcn_exp2f(x * x * -0.72134752044448170f);
+    float p = -0.06477917730808258f;
+    p = fmaf(p, t, 0.2428741753101349f);
+    p = fmaf(p, t, -0.256346195936203f);
+    p = fmaf(p, t, 0.2741190791130066f);
+    p = fmaf(p, t, -0.04752312600612640f);
+    p = fmaf(p, t, 0.10755722969770432f);
+    p = fmaf(p, t, 0.07414228469133377f);
+    p = fmaf(p, t, 0.0853620097041130f);
+    p = fmaf(p, t, 0.08459369838237762f);
+    return p * t;
 }
 
-template <class D>
+// (a NaN gives NaN in every branch)
+template <int ACT>
+__device__ __forceinline__ float act_value(float x) {
+    if constexpr (ACT == GTOPK_ACT_RELU) return x < 0.0f ? 0.0f : x;
+    if constexpr (ACT == GTOPK_ACT_TANH) return tanh_of(x);
+    if constexpr (ACT == GTOPK_ACT_SIGMOID) return logistic(x);
+    if constexpr (ACT == GTOPK_ACT_SILU) return x * logistic(x);
+    if constexpr (ACT == GTOPK_ACT_GELU) {
+        float bell;                                // x Phi(x) = max(x, 0) - |x| Phi(-|x|)
+        const float tail = normal_tail(x, bell);
+        return fmaf(-fabsf(x) * bell, tail, fmaxf(x, 0.0f));
+    }
+    return x;
+}
+template <int ACT>
+__device__ __forceinline__ float act_slope(float x) {
+    if constexpr (ACT == GTOPK_ACT_RELU) return x > 0.0f ? 1.0f : x <= 0.0f ? 0.0f : x;
+    if constexpr (ACT == GTOPK_ACT_TANH) {         // 1 - tanh^2 = 4 e / (1 + e)^2
+        const float e = exp_of(-2.0f * fabsf(x)), r = reciprocal(1.0f + e);
+        return 4.0f * e * r * r;
+    }
+    if constexpr (ACT == GTOPK_ACT_SIGMOID || ACT == GTOPK_ACT_SILU) {
+        const float e = exp_of(-fabsf(x)), r = reciprocal(1.0f + e), slope = e * r * r;
+        return ACT == GTOPK_ACT_SIGMOID ? slope : fmaf(x, slope, x < 0.0f ? e * r : r);
+    }
+    if constexpr (ACT == GTOPK_ACT_GELU) {
+        float bell;
+        const float below = normal_tail(x, bell) * bell;
+        return fmaf(x * 0.39894228040143268f, bell, x < 0.0f ? below : 1.0f - below);
+    }
+    return x == x ? 1.0f : x;
+}
+
+template <class D, int ACT>
 __global__ __launch_bounds__(kPackThreads) void k_unpack(
         const uint8_t* __restrict__ codes, int64_t code_stride, const uint8_t* __restrict__ scales, int64_t scale_stride,
-        PackGrid g, int act, typename D::T* __restrict__ out, int64_t stride) {
-    for_blocks(g, [&](int64_t row, uint32_t kb, int64_t col) {
+        PackGrid g, typename D::T* __restrict__ out, int64_t stride) {
+    constexpr int kRows = rows_ahead(sizeof(typename D::T));
+    uint32x2 c[kRows];
+    uint32_t s[kRows];
+    for_blocks<kRows>(g, [&](int u, int64_t row, uint32_t kb, int64_t col) {
+        c[u] = *reinterpret_cast<const uint32x2*>(codes + row * code_stride + col);
+        s[u] = scales[row * scale_stride + kb];
+    }, [&](int u, int64_t row, uint32_t, int64_t col) {
         float v[kLaneVals];
-        decode8(*reinterpret_cast<const uint32x2*>(codes + row * code_stride + col),
-                scale_value(scales[row * scale_stride + kb]), v);
+        decode8(c[u], scale_value(s[u]), v);
 #pragma unroll
-        for (int j = 0; j < kLaneVals; ++j) v[j] = act_value(act, v[j]);
-        const int64_t left = g.cols - col;
-        typename D::T* p = out + row * stride + col;
-        if (left >= kLaneVals) store8<D>(p, v);
-        else store_some<D>(p, (int)left, v);
+        for (int j = 0; j < kLaneVals; ++j) v[j] = act_value<ACT>(v[j]);
+        store_row<D>(out + row * stride + col, g.cols - col, v);
     });
 }
 
 // dx may be dy: a lane reads its values before it writes them, and nobody else touches them
-template <class D>
+template <class D, int ACT>
 __global__ __launch_bounds__(kPackThreads) void k_activation_grad(
         const uint8_t* __restrict__ codes, int64_t code_stride, const uint8_t* __restrict__ scales, int64_t scale_stride,
-        PackGrid g, int act, const typename D::T* dy, int64_t dy_stride, typename D::T* dx, int64_t dx_stride) {
-    for_blocks(g, [&](int64_t row, uint32_t kb, int64_t col) {
-        float v[kLaneVals], d[kLaneVals];
-        const int64_t left = g.cols - col;
-        const typename D::T* p = dy + row * dy_stride + col;
-        if (left >= kLaneVals) load8<D>(p, d);
-        else load_some<D>(p, (int)left, d);
-        decode8(*reinterpret_cast<const uint32x2*>(codes + row * code_stride + col),
-                scale_value(scales[row * scale_stride + kb]), v);
+        PackGrid g, const typename D::T* dy, int64_t dy_stride, typename D::T* dx, int64_t dx_stride) {
+    constexpr int kRows = rows_ahead(sizeof(typename D::T));
+    uint32x2 c[kRows];
+    uint32_t s[kRows];
+    Eight<D> in[kRows];
+    for_blocks<kRows>(g, [&](int u, int64_t row, uint32_t kb, int64_t col) {
+        in[u] = load_row<D>(dy + row * dy_stride + col, g.cols - col);
+        c[u] = *reinterpret_cast<const uint32x2*>(codes + row * code_stride + col);
+        s[u] = scales[row * scale_stride + kb];
+    }, [&](int u, int64_t row, uint32_t, int64_t col) {
+        float v[kLaneVals];
+        decode8(c[u], scale_value(s[u]), v);
 #pragma unroll
-        for (int j = 0; j < kLaneVals; ++j) d[j] *= act_slope(act, v[j]);
-        typename D::T* q = dx + row * dx_stride + col;
-        if (left >= kLaneVals) store8<D>(q, d);
-        else store_some<D>(q, (int)left, d);
+        for (int j = 0; j < kLaneVals; ++j) v[j] = (float)in[u][j] * act_slope<ACT>(v[j]);
+        store_row<D>(dx + row * dx_stride + col, g.cols - col, v);
     });
 }
 
