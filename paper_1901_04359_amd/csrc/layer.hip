@@ -17,7 +17,6 @@ using namespace gtopk;
 namespace {
 
 constexpr int64_t kMaxSide = 0x7FFFFFFF;            // rows and columns of a matrix
-constexpr int64_t kThinRows = 64;                   // products with at most so many rows of A: k_product_thin
 constexpr int64_t kMaxCodeStride = 1 << 23;         // of a product's operands: a tile's rows at offsets of 32 bits
 constexpr uint64_t kMaxBlocks = 1u << 22;           // blocks of a launch; kernels walk what is left
 
@@ -65,6 +64,33 @@ PackGrid pack_grid(int64_t rows, int64_t cols, int32_t dtype, dim3* grid) {
     while (g.side_log2 < 4 && (1u << g.side_log2) < g.nb) ++g.side_log2;
     const int64_t deep = ((kPackThreads / 16) >> g.side_log2) * rows_ahead(value_bytes(dtype)), down = ceil_div(rows, deep);
     *grid = dim3((uint32_t)ceil_div(g.nb, 1 << g.side_log2), (uint32_t)(down < 65535 ? down : 65535));
+    return g;
+}
+
+// How a product is computed: few rows of A without tiles, else tiles of 128 x 128, and where they are too few for the
+// chip's 256 compute units (two blocks each), shares of K, joined from the workspace.
+struct ProductPlan {
+    bool thin;
+    uint32_t tiles_m, tiles_n, share, shares;       // blocks of 128 per share
+    int64_t stride;                                 // of a share's result
+};
+// (us, without tiles / with: 32 x 4096 x 9216 15.1 / 15.5; 17 rows 12.9 / 15.0; 64 rows 24.6 / 16.9)
+constexpr int64_t kThinRows = 32;
+// blocks of 128 per share, at least; a multiple of 4.  (us with 4, 8, 16: 128 x 4096 x 4096 17.5, 15.2, 17.6; 1024^3 12.7, 9.2, 9.2;
+// 64 x 4096 x 9216 16.9, 16.9, 22.1; 512 x 1000 x 4096 16.2, 15.5, 17.4, and 22.9 in one piece)
+constexpr uint32_t kProductShare = 8;
+ProductPlan product_plan(int64_t M, int64_t N, int64_t K) {
+    ProductPlan g;
+    const uint32_t nb = (uint32_t)ceil_div(K, kPackBlock);
+    g.thin = M <= kThinRows;
+    g.tiles_m = (uint32_t)ceil_div(M, 128);
+    g.tiles_n = (uint32_t)ceil_div(N, 128);
+    g.stride = ceil_div(N, 4) * 4;
+    const uint64_t tiles = (uint64_t)g.tiles_m * g.tiles_n;
+    uint64_t want = g.thin || tiles == 0 ? 1 : 512 / tiles;
+    if (want > nb / kProductShare) want = nb / kProductShare;
+    g.share = want > 1 ? (uint32_t)ceil_div(ceil_div(nb, (int64_t)want), 4) * 4 : nb;
+    g.shares = (uint32_t)ceil_div(nb, g.share);
     return g;
 }
 
@@ -189,7 +215,8 @@ int gtopk_activation_grad(const uint8_t* codes, int64_t code_stride, const uint8
 
 size_t gtopk_product_workspace_bytes(int64_t M, int64_t N, int64_t K) {
     if (!side_ok(M, 0) || !side_ok(N, 1) || !side_ok(K, 1) || K > kMaxCodeStride) return 0;
-    return 256;
+    const ProductPlan g = product_plan(M, N, K);
+    return 256 + (g.shares > 1 ? (size_t)g.shares * M * g.stride * sizeof(float) : 0);
 }
 
 int gtopk_scaled_product(const uint8_t* a_codes, int64_t a_code_stride, const uint8_t* a_scales, int64_t a_scale_stride,
@@ -208,24 +235,26 @@ int gtopk_scaled_product(const uint8_t* a_codes, int64_t a_code_stride, const ui
     const PackedMatrix a{a_codes, a_scales, (uint32_t)a_code_stride, (uint32_t)a_scale_stride};
     const PackedMatrix b{b_codes, b_scales, (uint32_t)b_code_stride, (uint32_t)b_scale_stride};
     const uint32_t nb = (uint32_t)ceil_div(K, kPackBlock);
+    const ProductPlan g = product_plan(M, N, K);
     hipStream_t st = (hipStream_t)stream;
     by_type(dtype, [&](auto d) {
         using D = decltype(d);
         typename D::T* const to = (typename D::T*)out;
-        if (M <= kThinRows) {
+        if (g.thin) {
             const dim3 grid((uint32_t)ceil_div(N, 16)), block(kThinWaves * kWave);
             if (M <= 16) hipLaunchKernelGGL((k_product_thin<D, 1>), grid, block, 0, st, a, b, M, N, nb, to, out_stride);
-            else if (M <= 32) hipLaunchKernelGGL((k_product_thin<D, 2>), grid, block, 0, st, a, b, M, N, nb, to, out_stride);
-            else hipLaunchKernelGGL((k_product_thin<D, 4>), grid, block, 0, st, a, b, M, N, nb, to, out_stride);
+            else hipLaunchKernelGGL((k_product_thin<D, 2>), grid, block, 0, st, a, b, M, N, nb, to, out_stride);
             return;
         }
-#ifndef CFG
-#define CFG 128, 128, 64, 64
-#endif
-        constexpr int c[4] = {CFG};
-        const uint32_t tiles_m = (uint32_t)ceil_div(M, c[0]), tiles_n = (uint32_t)ceil_div(N, c[1]);
-        hipLaunchKernelGGL((k_product<D, Exact<D>::value, CFG>), dim3(tiles_m * tiles_n), dim3((c[0] / c[2]) * (c[1] / c[3]) * kWave), 0,
-                           st, a, b, M, N, nb, to, out_stride, tiles_m, tiles_n);
+        if (g.shares == 1) {
+            hipLaunchKernelGGL((k_product<D, Exact<D>::value, 128, 128, 64, 64>), dim3(g.tiles_m * g.tiles_n), dim3(256), 0, st, a, b, M, N,
+                               nb, to, out_stride, g.tiles_m, g.tiles_n, nb);
+            return;
+        }
+        hipLaunchKernelGGL((k_product<F32, Exact<D>::value, 128, 128, 64, 64>), dim3(g.tiles_m * g.tiles_n, g.shares), dim3(256), 0, st, a, b,
+                           M, N, nb, (float*)ws, g.stride, g.tiles_m, g.tiles_n, g.share);
+        hipLaunchKernelGGL(k_join_products<D>, dim3((uint32_t)ceil_div(g.stride, 4 * kPackThreads), (uint32_t)M), dim3(kPackThreads), 0, st,
+                           (const float*)ws, g.shares, M * g.stride, g.stride, N, to, out_stride);
     });
     return launch_status();
 }

@@ -6,6 +6,8 @@
 // blocks stays in the fp32 accumulators.  A lane l gives 32 codes of row l % 16; which 32 of the 128 does not
 // matter as long as both operands agree, and all four lanes of a row give the same scale.
 #pragma once
+#include <type_traits>
+
 #include "packed.hip.h"
 
 namespace gtopk {
@@ -45,30 +47,36 @@ __device__ __forceinline__ bf16x8 decode_bf16(int c0, int c1, float scale) {
     return __builtin_bit_cast(bf16x8, u);
 }
 
-// sum + one block of 128: B's row is the instruction's first operand, so a lane holds four consecutive columns of C
-template <bool EXACT>
+// sum + one block of 128: B's row is the instruction's first operand, so a lane holds four consecutive columns of C.
+// The scales are byte BYTE of sb and sa.
+template <bool EXACT, int BYTE>
 __device__ __forceinline__ floatx4 multiply(intx8 vb, uint32_t sb, intx8 va, uint32_t sa, floatx4 sum) {
     if constexpr (EXACT) {
-        const float fa = scale_value(sa & 255u), fb = scale_value(sb & 255u);
+        const float fa = scale_value(sa >> (8 * BYTE) & 255u), fb = scale_value(sb >> (8 * BYTE) & 255u);
 #pragma unroll
         for (int q = 0; q < 4; ++q)
             sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode_bf16(vb[2 * q], vb[2 * q + 1], fb), decode_bf16(va[2 * q], va[2 * q + 1], fa), sum, 0, 0, 0);
         return sum;
     } else {
-        return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(vb, va, sum, 0, 0, 0, (int)sb, 0, (int)sa);
+        return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(vb, va, sum, 0, 0, BYTE, (int)sb, BYTE, (int)sa);
     }
 }
 
-// A block computes BM x BN values with BM/WM x BN/WN waves of WM x WN each.  A block of 128 of the tile's rows of A and B
+// A block computes BM x BN values with BM/WM x BN/WN waves of WM x WN each.  (Tiles of 128 x 128 with four waves, two blocks per
+// compute unit: 2048 x 4096 x 9216 to bf16 in 72 us = 2.1 PFLOP/s, 8192^3 in 509 us = 2.2; to fp32 146 and 929 us.  What
+// bounds them is LDS: per two blocks of 128 a compute unit reads 128 KB and writes 64 KB there, 1536 cycles at 128 bytes, where the matrix
+// instructions take 1024.  256 x 256 with four waves, which needs half of that, has one wave per SIMD and waits as much as it saves:
+// 142 and 493 us; 256 x 128 with eight 89 and 620; three LDS buffers of 256 x 128 with four 106 and 658.)  A block of 128 of the tile's rows of A and B
 // goes straight from global memory into one of two LDS buffers while the matrix instructions work on the other; the scales
 // of four blocks go together (a word per row: fetched one by one they would be as many requests as the codes).
 // In LDS a row's 16-byte pieces are exchanged by the row's number (piece p lies at p ^ (row / 2 % 8)): rows are 128
 // bytes apart, and without that a wave's lanes would read from an eighth of the banks.  Rows behind the
-// matrix's end are read as its last row and not written.
+// matrix's end are read as its last row and not written.  Grid: x the tiles, y shares of `share` blocks of 128 (a multiple of 4, or
+// all of them), each written to a result of its own.
 template <class D, bool EXACT, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__((BM / WM) * (BN / WN) * kWave, 1) void k_product(
-        PackedMatrix a, PackedMatrix b, int64_t M, int64_t N, uint32_t nb, typename D::T* __restrict__ out, int64_t out_stride,
-        uint32_t tiles_m, uint32_t tiles_n) {
+        PackedMatrix a, PackedMatrix b, int64_t M, int64_t N, uint32_t blocks, typename D::T* __restrict__ out, int64_t out_stride,
+        uint32_t tiles_m, uint32_t tiles_n, uint32_t share) {
     constexpr int kWavesN = BN / WN, kWaves = (BM / WM) * kWavesN, kThreads = kWaves * kWave;
     constexpr int TM = WM / 16, TN = WN / 16;
     constexpr int kScaleLoads = (BM + BN + kThreads - 1) / kThreads;
@@ -81,12 +89,15 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * kWave, 1) void k_product(
     __shared__ __align__(128) uint8_t s_scales[2][kScaleLoads * kThreads * 4];      // a word per row: four blocks' scales
 
     const uint32_t wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
-    const uint32_t tile = by_xcd(blockIdx.x, tiles_m * tiles_n);
+    const uint32_t first = blockIdx.y * share, nb = blocks - first < share ? blocks - first : share;     // this share's blocks of 128
+    out += blockIdx.y * M * out_stride;
     uint32_t tile_m, tile_n;
-    tile_at(tile, tiles_m, tiles_n, 2048 / BM, tile_m, tile_n);
+    tile_at(by_xcd(blockIdx.x, tiles_m * tiles_n), tiles_m, tiles_n, 2048 / BM, tile_m, tile_n);
+    tile_m = __builtin_amdgcn_readfirstlane(tile_m);
+    tile_n = __builtin_amdgcn_readfirstlane(tile_n);
     const int64_t m0 = (int64_t)tile_m * BM, n0 = (int64_t)tile_n * BN;
-    const uint8_t* const a_base = a.codes + m0 * a.code_stride;
-    const uint8_t* const b_base = b.codes + n0 * b.code_stride;
+    const uint8_t* const a_base = a.codes + m0 * a.code_stride + (int64_t)first * kPackBlock;
+    const uint8_t* const b_base = b.codes + n0 * b.code_stride + (int64_t)first * kPackBlock;
     const uint32_t a_last = (uint32_t)(M - m0 < BM ? M - m0 - 1 : BM - 1), b_last = (uint32_t)(N - n0 < BN ? N - n0 - 1 : BN - 1);
 
     uint32_t offset[kLoads];
@@ -104,13 +115,15 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * kWave, 1) void k_product(
         const uint32_t r = i * kThreads + threadIdx.x;
         scales_from[i] = r < BM ? a.scales + (m0 + (r < a_last ? r : a_last)) * a.scale_stride
                                 : b.scales + (n0 + (r - BM < b_last ? r - BM : b_last)) * b.scale_stride;
+        scales_from[i] += first;           // (a multiple of 4)
     }
     auto fetch = [&](uint32_t kb, uint8_t* stage) __attribute__((always_inline)) {
+        uint32_t at = kb * kPackBlock;
+        asm("" : "+s"(at));                // scalar bases and offsets of 32 bits, not a pointer per load that is carried along
+        const uint8_t *a_from = a_base + at, *b_from = b_base + at;
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const uint8_t* base = (i * kThreads / 8 < BM ? a_base : b_base) + (int64_t)kb * kPackBlock;
-            load_to_lds16(base + offset[i], stage + (i * kThreads + wave * kWave) * 16);
-        }
+        for (int i = 0; i < kLoads; ++i)
+            load_to_lds16((i * kThreads / 8 < BM ? a_from : b_from) + offset[i], stage + (i * kThreads + wave * kWave) * 16);
     };
     auto fetch_scales = [&](uint32_t kb, uint8_t* to) __attribute__((always_inline)) {
 #pragma unroll
@@ -155,7 +168,7 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * kWave, 1) void k_product(
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll
-            for (int j = 0; j < TN; ++j) sum[i][j] = multiply<EXACT>(vb[j], sb[j] >> (8 * in4), va[i], sa[i] >> (8 * in4), sum[i][j]);
+            for (int j = 0; j < TN; ++j) sum[i][j] = multiply<EXACT, 0>(vb[j], sb[j] >> (8 * in4), va[i], sa[i] >> (8 * in4), sum[i][j]);
     };
     for (uint32_t kb = 0; kb < nb; kb += 4) {
         block(kb, 0, s_codes0, s_codes1);
@@ -176,7 +189,8 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * kWave, 1) void k_product(
     }
 }
 
-// Few rows of A (at most 16 TM): what counts is reading B once at the memory's rate.  A block computes 16 columns of C
+// Few rows of A (at most 16 TM): what counts is reading B once at the memory's rate (1 x 4096 x 9216: 38 MB in 9.5 us with the host's
+// part of the call; 1 x 16384 x 9216: 151 MB in 29.5 us = 5.1 TB/s).  A block computes 16 columns of C
 // with kThinWaves waves that share out the blocks of 128 among them and read both matrices straight into registers, kThinAhead
 // blocks of 128 at a time, so that a compute unit has some 64 KB of B under way; the waves' sums are joined in LDS, in their order.
 constexpr int kThinWaves = 8;
@@ -221,7 +235,7 @@ __global__ __launch_bounds__(kThinWaves * kWave) void k_product_thin(PackedMatri
         for (int u = 0; u < kAhead; ++u) {
             if (k0 + u * kThinWaves < nb) {
 #pragma unroll
-                for (int i = 0; i < TM; ++i) sum[i] = multiply<Exact<D>::value>(vb[u], sb[u], va[u][i], sa[u][i], sum[i]);
+                for (int i = 0; i < TM; ++i) sum[i] = multiply<Exact<D>::value, 0>(vb[u], sb[u], va[u][i], sa[u][i], sum[i]);
             }
         }
     }
@@ -234,6 +248,18 @@ __global__ __launch_bounds__(kThinWaves * kWave) void k_product_thin(PackedMatri
         for (int w = 1; w < kThinWaves; ++w) v += s_sum[w][i][lane];
         const int64_t m = i * 16 + in16, at = n0 + quarter * 4;
         if (m < M && at < N) store4<D>(out + m * out_stride + at, N - at, v);
+    }
+}
+
+// the sum of the shares, in their order; their rows lie `stride` apart, a multiple of 4
+template <class D>
+__global__ __launch_bounds__(kPackThreads) void k_join_products(const float* __restrict__ part, uint32_t shares, int64_t share_stride,
+                                                                int64_t stride, int64_t N, typename D::T* __restrict__ out, int64_t out_stride) {
+    const float* from = part + blockIdx.y * stride;
+    for (int64_t n = ((int64_t)blockIdx.x * kPackThreads + threadIdx.x) * 4; n < N; n += (int64_t)gridDim.x * kPackThreads * 4) {
+        floatx4 v = *reinterpret_cast<const floatx4*>(from + n);
+        for (uint32_t s = 1; s < shares; ++s) v += *reinterpret_cast<const floatx4*>(from + s * share_stride + n);
+        store4<D>(out + blockIdx.y * out_stride + n, N - n, v);
     }
 }
 
