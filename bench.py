@@ -186,6 +186,90 @@ def time_aggregations(B, torch, cfg, grads, reps: int = 20):
     }
 
 
+def time_backward(B, torch, W, cfg, samples: int, reps: int = 10):
+    """The layer calls before the hot path on the fully connected layers of the AlexNet workload (those that fit a row
+    of this workload), `samples` samples per worker: weights packed after an update, forward products, activation
+    checkpoints, input gradients, and every worker's weight gradients written into the end of its gradient row; then
+    gtopk_step on those rows.  HIP events, `reps` repetitions of each."""
+    P, m, k = cfg.P, cfg.m, cfg.k
+    layers, at, end = [], [], m
+    for n, kk in reversed(W.FC_LAYERS):                  # the last layer ends the row
+        if end < n * kk:
+            break
+        end -= n * kk
+        layers.insert(0, (n, kk))
+        at.insert(0, end)
+    if not layers:
+        return {"note": "no fully connected layer fits this workload's rows"}
+    R, dev = P * samples, "cuda"
+    gen = torch.Generator(device=dev)
+    gen.manual_seed(W.BASE_SEED)
+    grads, res = torch.zeros((P, m), device=dev), torch.zeros((P, m), device=dev)
+    grads.normal_(generator=gen).mul_(1e-4)              # the layers before the fully connected ones
+    weights = torch.randn(m, device=dev, generator=gen) * 0.01
+    rows = lambda i: grads[:, at[i]:at[i] + layers[i][0] * layers[i][1]].unflatten(1, layers[i])
+    weight = lambda i: weights[at[i]:at[i] + layers[i][0] * layers[i][1]].view(layers[i])
+    x = torch.randn((R, layers[0][1]), device=dev, generator=gen).relu_().bfloat16()
+    y = [torch.empty((R, n), dtype=torch.bfloat16, device=dev) for n, _ in layers]
+    dy = [torch.empty((R, n), dtype=torch.bfloat16, device=dev) for n, _ in layers]
+    dy[-1].copy_(torch.randn(dy[-1].shape, device=dev, generator=gen) * 1e-3)
+    w, wt = [B.alloc_packed(n, kk) for n, kk in layers], [B.alloc_packed(kk, n) for n, kk in layers]
+    cx, cy = [B.alloc_packed(R, kk) for _, kk in layers], [B.alloc_packed(R, n) for n, _ in layers]
+    ws_f = [B.alloc_product_workspace(R, n, kk) for n, kk in layers]
+    ws_b = [B.alloc_product_workspace(R, kk, n) for n, kk in layers]
+    ws_w = [B.alloc_weight_grad_workspace(R, P, n, kk) for n, kk in layers]
+    g_idx, g_val = torch.zeros(k, dtype=torch.int32, device=dev), torch.zeros(k, device=dev)
+    ws = B.alloc_workspace(m, k, P)
+    L = range(len(layers))
+
+    def pack_weights():
+        for i in L:
+            B.gtopk_pack_tiles(weight(i), *w[i], *wt[i])
+
+    def forward():
+        B.gtopk_pack_rows(x, *cx[0])
+        for i in L:
+            B.gtopk_scaled_product(*cx[i], *w[i], layers[i][1], y[i], ws_f[i])
+            if i + 1 < len(layers):                      # the checkpoint of what goes into the ReLU, and the next layer's input
+                B.gtopk_pack_rows(y[i], *cy[i])
+                B.gtopk_unpack(*cy[i], "relu", y[i])
+                B.gtopk_pack_rows(y[i], *cx[i + 1])
+
+    def input_gradients():
+        for i in reversed(L):
+            if i > 0:
+                B.gtopk_pack_rows(dy[i], *cy[i])
+                B.gtopk_scaled_product(*cy[i], *wt[i], layers[i][0], dy[i - 1], ws_b[i])
+                B.gtopk_activation_grad(*cx[i], "relu", dy[i - 1], dy[i - 1])
+
+    def weight_gradients():
+        for i in L:
+            B.gtopk_weight_grad(dy[i], *cx[i], None, rows(i), False, ws_w[i])
+
+    def step():
+        B.gtopk_step(grads, res, k, g_idx, g_val, None, None, ws)
+
+    def timed(fn):
+        fn()
+        torch.cuda.synchronize()
+        e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        e0.record()
+        for _ in range(reps):
+            fn()
+        e1.record()
+        torch.cuda.synchronize()
+        return round(e0.elapsed_time(e1) / reps, 4)
+
+    flops = 2.0 * R * sum(n * kk for n, kk in layers)
+    t_w, t_f, t_i, t_g, t_s = (timed(f) for f in (pack_weights, forward, input_gradients, weight_gradients, step))
+    return {"layers": [f"{kk}->{n}" for n, kk in layers], "samples_per_worker": samples, "workers": P,
+            "pack_weights_ms": t_w, "forward_ms": t_f, "forward_TFLOPs": round(flops / t_f / 1e9, 1),
+            "input_gradients_ms": t_i, "weight_gradients_ms": t_g,
+            "weight_gradients_written_GBs": round(4.0 * P * sum(n * kk for n, kk in layers) / t_g / 1e6, 1),
+            "gtopk_step_on_these_rows_ms": t_s,
+            "note": "bf16 activations and output gradients, random data; checkpoints and products in 8 bits"}
+
+
 def time_three_calls(B, torch, cfg, grads, res, g_idx, g_val, ws, reps: int = 10):
     """gtopk_local_select, gtopk_tree and gtopk_residual_restore timed one by one (HIP events,
     `reps` repetitions each; the residual keeps evolving, as in training)."""
@@ -262,6 +346,10 @@ def main() -> int:
     ap.add_argument("--aggregations", action="store_true",
                     help="also time the paper's comparison aggregations (Algorithms 1 and 2) "
                          "against the tree on this workload's local sets")
+    ap.add_argument("--backward", type=int, default=0, metavar="SAMPLES",
+                    help="also time the layer calls before the hot path (packed activations, scaled products, "
+                         "weight gradients into the workers' rows) with so many samples per worker, on the "
+                         "AlexNet workload's fully connected layers that fit this workload's rows")
     ap.add_argument("--degenerate-workers", type=int, default=0,
                     help="replace the gradient rows of this many workers by rows of equal "
                          "magnitudes, which overflow the candidate list and are selected from "
@@ -449,6 +537,10 @@ def main() -> int:
     if args.per_iteration:
         del res, ws, grads
         out["per_iteration"] = time_per_iteration(B, torch, W, cfg)
+    if args.backward > 0:
+        grads = res = ws = None
+        torch.cuda.empty_cache()
+        out["backward"] = time_backward(B, torch, W, cfg, args.backward)
     if args.cpu_workers != 0:
         out["cpu_baseline"] = cpu_baseline(cfg, args.cpu_workers)
     print(json.dumps(out))

@@ -62,6 +62,10 @@ CONFIGS: Dict[str, Config] = {
 }
 
 
+# (outputs, inputs) of the fully connected layers that the three trailing segments of the AlexNet-sized workload stand for
+FC_LAYERS: Tuple[Tuple[int, int], ...] = ((4096, 9216), (4096, 4096), (1000, 4096))
+
+
 def _rng(cid: int, stream: int, a: int = 0, b: int = 0) -> np.random.Generator:
     # Philox takes a 2x64-bit key; fold the five words into it reproducibly.
     k0 = (BASE_SEED << 20) ^ (cid << 8) ^ stream
