@@ -32,6 +32,7 @@
  *   - Return value: GTOPK_OK (0) when the work was enqueued, a negative
  *     gtopk_status otherwise; on an argument error nothing is enqueued.
  *     Argument errors are found on the host, without touching the GPU.
+ *     (Calls of the layer section state their own types, alignments and what they do with NaN and Inf.)
  *   - Not checked (results unspecified, but no access outside the given sizes):
  *     NaN/Inf inputs; unsorted, duplicate or out-of-range indices in
  *     caller-provided k-sets (an entry whose index is >= m is skipped where it
@@ -55,9 +56,12 @@ typedef enum {
                               a power of two (the paper assumes a power of two, Section III);
                               stride < m; batch < 1 or batch > 32767; k-set stride < k;
                               copies < 1 or > 65535 (gtopk_apply_update); P > 1024
-                              (gtopk_topk_allreduce, which takes any P from 1 on)            */
+                              (gtopk_topk_allreduce, which takes any P from 1 on); the layer calls:
+                              an unknown dtype or act, sizes and strides outside what the call states,
+                              rows that P does not divide (gtopk_weight_grad without row_begin)  */
     GTOPK_EWORKSPACE = -2, /* ws_bytes smaller than the matching *_workspace_bytes query   */
-    GTOPK_EALIGN = -3,     /* a pointer is not 16-byte aligned                              */
+    GTOPK_EALIGN = -3,     /* a pointer is not 16-byte aligned (the layer calls: dense matrices to one
+                              value, scales and row_begin to 4 bytes)                        */
     GTOPK_EHIP = -4        /* a kernel launch failed (hipGetLastError)                      */
 } gtopk_status;
 
@@ -316,7 +320,8 @@ int gtopk_activation_grad(const uint8_t* codes, int64_t code_stride, const uint8
  *   GTOPK_F32:  products are exact, sums are fp32 (magnitudes below 2^-126 may be rounded to a multiple of 2^-133).
  *   GTOPK_BF16, GTOPK_F16: twice as fast.  The eight products of k = 8 j .. 8 j + 7 are exact, but each is cut
  *               off at 2^-13 of the largest of the eight (its leading bit); all further sums are fp32.
- *   Code strides (and so K) of at most 2^23.
+ *   Strides of codes and scales (and so K) of at most 2^23; fewer than 2^24 tiles of 128 x 128 in out, for M <= 32
+ *   N of at most 2^26.
  *   ws : gtopk_product_workspace_bytes(M, N, K) bytes (0 if the sizes are invalid)
  */
 size_t gtopk_product_workspace_bytes(int64_t M, int64_t N, int64_t K);

@@ -17,7 +17,9 @@ using namespace gtopk;
 namespace {
 
 constexpr int64_t kMaxSide = 0x7FFFFFFF;            // rows and columns of a matrix
-constexpr int64_t kMaxCodeStride = 1 << 23;         // of a product's operands: a tile's rows at offsets of 32 bits
+constexpr int64_t kMaxCodeStride = 1 << 23;         // of a product's operands (also of their scales): a tile's rows at offsets of 32 bits
+constexpr int64_t kMaxTiles = (1 << 24) - 1;        // blocks of a product: fewer than 2^32 threads in a launch
+constexpr int64_t kMaxThinColumns = 1 << 26;
 constexpr uint64_t kMaxBlocks = 1u << 22;           // blocks of a launch; kernels walk what is left
 
 inline bool aligned(const void* p, size_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
@@ -216,6 +218,7 @@ int gtopk_activation_grad(const uint8_t* codes, int64_t code_stride, const uint8
 size_t gtopk_product_workspace_bytes(int64_t M, int64_t N, int64_t K) {
     if (!side_ok(M, 0) || !side_ok(N, 1) || !side_ok(K, 1) || K > kMaxCodeStride) return 0;
     const ProductPlan g = product_plan(M, N, K);
+    if (g.thin ? N > kMaxThinColumns : (int64_t)g.tiles_m * g.tiles_n > kMaxTiles) return 0;
     return 256 + (g.shares > 1 ? (size_t)g.shares * M * g.stride * sizeof(float) : 0);
 }
 
@@ -226,7 +229,8 @@ int gtopk_scaled_product(const uint8_t* a_codes, int64_t a_code_stride, const ui
     const size_t need = gtopk_product_workspace_bytes(M, N, K);
     if (!need || !dtype_ok(dtype) || out_stride < N) return GTOPK_EINVAL;
     if (!packed_strides_ok(K, a_code_stride, a_scale_stride) || !packed_strides_ok(K, b_code_stride, b_scale_stride)) return GTOPK_EINVAL;
-    if (a_code_stride > kMaxCodeStride || b_code_stride > kMaxCodeStride) return GTOPK_EINVAL;
+    if (a_code_stride > kMaxCodeStride || b_code_stride > kMaxCodeStride || a_scale_stride > kMaxCodeStride || b_scale_stride > kMaxCodeStride)
+        return GTOPK_EINVAL;
     if (M == 0) return GTOPK_OK;
     if (!a_codes || !a_scales || !b_codes || !b_scales || !out || !ws) return GTOPK_EINVAL;
     if (!packed_aligned(a_codes, a_scales) || !packed_aligned(b_codes, b_scales) || !aligned(out, value_bytes(dtype)) || !aligned(ws, 16))

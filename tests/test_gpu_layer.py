@@ -328,6 +328,42 @@ def test_product_with_nan_and_extreme_scales(M, N, K):
     assert torch.equal(out.cpu(), torch.from_numpy(ref.values(*a, K) @ ref.values(*b, K).T).float())
 
 
+@pytest.mark.parametrize("M,N,K", [(3, 40, 500), (40, 30, 1100), (130, 140, 300)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_product_of_scales_over_their_whole_range(M, N, K, dtype):
+    """Blocks of every scale that pack makes, in pairs whose product is near 1: sums are exact in every type's path."""
+    import torch
+    from paper_1901_04359_amd import binding as B
+    t = torch_type(dtype)
+    a, b = int_packed(M, K, 13), int_packed(N, K, 14)
+    r = np.random.default_rng([M, N, K])
+    nb = -(-K // 128)
+    each = r.integers(7, 248, nb)                             # A's, per block; B's make up for it: 7 .. 247 as well
+    a[1][:] = each[None, :]
+    b[1][:] = np.clip(254 - each, 7, 247)[None, :]
+    want = torch.from_numpy(ref.values(*a, K) @ ref.values(*b, K).T)
+    out = torch.zeros(M, N, dtype=t, device="cuda")
+    say(f"layer: product {M}x{N}x{K} {dtype}, all scales")
+    B.gtopk_scaled_product(*packed_on_gpu(*a), *packed_on_gpu(*b), K, out, B.alloc_product_workspace(M, N, K))
+    assert torch.equal(out.cpu(), want.float().to(t))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_product_with_nan_in_16_bits(dtype):
+    import torch
+    from paper_1901_04359_amd import binding as B
+    t = torch_type(dtype)
+    for M, N, K in ((3, 40, 500), (130, 140, 300)):
+        a, b = int_packed(M, K, 3), int_packed(N, K, 4)
+        a[0][1, 7], b[0][N - 1, K - 1], b[1][N - 2, 0] = 0x7F, 0xFF, 255
+        out = torch.zeros(M, N, dtype=t, device="cuda")
+        say(f"layer: product {M}x{N}x{K} {dtype} with NaN")
+        B.gtopk_scaled_product(*packed_on_gpu(*a), *packed_on_gpu(*b), K, out, B.alloc_product_workspace(M, N, K))
+        want = torch.from_numpy(ref.values(*a, K) @ ref.values(*b, K).T).float().to(t)
+        assert torch.equal(torch.isnan(out.cpu()), torch.isnan(want))
+        assert torch.equal(torch.nan_to_num(out.cpu()), torch.nan_to_num(want))
+
+
 # ---- weight gradient ------------------------------------------------------------------
 
 def begins(P, rows, kind, seed=0):
@@ -456,6 +492,59 @@ def test_row_begin_out_of_range_stays_inside():
     x = ref.values(codes, scales, K)
     want = np.stack([dy[a:b].T @ x[a:b] for a, b in ((0, 10), (10, 10), (7, 30), (30, 30))])
     assert torch.equal(grad.cpu(), torch.from_numpy(want).float())
+
+
+def test_offsets_past_32_bits():
+    """Matrices of more than 2^32 bytes, gradient rows more than 2^32 bytes apart: the far ends against the near ones."""
+    import torch
+    from paper_1901_04359_amd import binding as B
+    rows, cols, tail = 560_000, 8192, 130
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(5)
+    x = torch.empty(rows, cols, dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+    codes, scales = B.alloc_packed(rows, cols)
+    assert codes.numel() > 2**32
+    say("layer: pack past 2^32")
+    B.gtopk_pack_rows(x, codes, scales)
+    want_c, want_s = ref.pack(x[-tail:].double().cpu().numpy())
+    assert np.array_equal(codes[-tail:].cpu().numpy(), want_c) and np.array_equal(scales[-tail:].cpu().numpy(), want_s)
+    far, near = torch.empty(rows, cols, dtype=torch.bfloat16, device="cuda"), torch.empty(tail, cols, dtype=torch.bfloat16, device="cuda")
+    c, s = codes[-tail:].clone(), scales[-tail:].clone()
+    say("layer: unpack and gradient past 2^32")
+    B.gtopk_unpack(codes, scales, "silu", far)
+    B.gtopk_unpack(c, s, "silu", near)
+    assert torch.equal(far[-tail:], near)
+    B.gtopk_activation_grad(codes, scales, "silu", x, x)
+    dy = torch.empty(tail, cols, dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+    far[-tail:] = dy
+    B.gtopk_activation_grad(c, s, "silu", dy, near)
+    B.gtopk_activation_grad(codes, scales, "silu", far, far)
+    assert torch.equal(far[-tail:], near)
+    del far, near, x
+    b = B.alloc_packed(40, cols)
+    B.gtopk_pack_rows(torch.empty(40, cols, device="cuda").normal_(generator=gen), *b)
+    say("layer: product past 2^32")
+    out, part = torch.empty(rows, 40, device="cuda"), torch.empty(tail, 40, device="cuda")
+    B.gtopk_scaled_product(codes, scales, *b, cols, out, B.alloc_product_workspace(rows, 40, cols))
+    B.gtopk_scaled_product(c, s, *b, cols, part, B.alloc_product_workspace(tail, 40, cols))
+    size = part.abs().max()
+    assert bool(((out[-tail:] - part).abs() <= cols * 2.0 ** -22 * size).all())      # the near one is summed in shares of K
+    # the last rows as one of three workers, whose gradients lie 6 GB apart
+    N = 12
+    d = torch.empty(rows, N, dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+    grads = torch.empty(3, 1_500_000_000, device="cuda")
+    grad = grads[:, 7:7 + N * cols].unflatten(1, (N, cols))
+    plan = torch.tensor([0, 100, 100, rows], dtype=torch.int32, device="cuda")
+    plan[2] = rows - tail
+    say("layer: weight_grad past 2^32")
+    B.gtopk_weight_grad(d, codes, scales, plan, grad, False, B.alloc_weight_grad_workspace(rows, 3, N, cols))
+    one = torch.empty(1, N, cols, device="cuda")
+    B.gtopk_weight_grad(d[-tail:], c, s, None, one, False, B.alloc_weight_grad_workspace(tail, 1, N, cols))
+    size = one.abs().max()
+    assert bool(((grad[2] - one[0]).abs() <= tail * 2.0 ** -22 * size).all())
+    want = d[:100].float().t() @ (codes[:100].view(torch.float8_e4m3fn).float() *
+                                  torch.exp2(scales[:100, :cols // 128].float() - 127).repeat_interleave(128, dim=1))
+    assert bool(((grad[0] - want).abs() <= 200 * 2.0 ** -22 * want.abs().max()).all())
 
 
 # ---- together, on streams, in graphs --------------------------------------------------

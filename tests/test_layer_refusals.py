@@ -65,13 +65,14 @@ def test_unpack_and_activation_grad():
 def test_scaled_product():
     ws = B.gtopk_product_workspace_bytes(5, 7, 130)
     assert ws > 0 and B.gtopk_product_workspace_bytes(0, 7, 130) > 0
-    for bad in ((-1, 7, 130), (5, 0, 130), (5, 7, 0), (2**31, 7, 130), (5, 2**31, 130), (5, 7, 2**31), (5, 7, 2**23 + 1)):
+    for bad in ((-1, 7, 130), (5, 0, 130), (5, 7, 0), (2**31, 7, 130), (5, 2**31, 130), (5, 7, 2**31), (5, 7, 2**23 + 1), (32, 2**26 + 1, 8),
+                (2**31 - 1, 1, 1), (2**19, 2**19, 1)):
         assert B.gtopk_product_workspace_bytes(*bad) == 0
     f = call("gtopk_scaled_product", dict(a=FAKE, acs=256, asc=FAKE, ass=4, b=FAKE, bcs=256, bsc=FAKE, bss=4, M=5, N=7, K=130,
                                           out=FAKE, dtype=0, os=7, ws=FAKE, wsb=ws, st=None))
     for kw in (dict(a=None), dict(asc=None), dict(b=None), dict(bsc=None), dict(out=None), dict(ws=None), dict(M=-1), dict(N=0), dict(K=0),
                dict(acs=128), dict(bcs=128), dict(acs=257), dict(ass=1), dict(bss=7), dict(dtype=3), dict(os=6), dict(acs=2**23 + 128),
-               dict(bcs=2**23 + 128)):
+               dict(bcs=2**23 + 128), dict(ass=2**23 + 4), dict(bss=2**23 + 4)):
         assert f(**kw) == EINVAL, kw
     for kw in (dict(a=ODD), dict(b=ODD), dict(asc=UNEVEN), dict(bsc=UNEVEN), dict(out=UNEVEN), dict(ws=ODD)):
         assert f(**kw) == EALIGN, kw
