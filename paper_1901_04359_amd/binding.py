@@ -135,7 +135,9 @@ def gtopk_merge_workspace_bytes(k: int, batch: int) -> int:
 # -- marshalling helpers ------------------------------------------------------
 
 def _torch():
+    global _torch_module
     import torch
+    _torch_module = torch
     return torch
 
 
@@ -434,6 +436,8 @@ def gtopk_debug_candidate_counts(ws, m: int, k: int, P: int):
 # GPU, and the call runs there, on that GPU's current stream.  The smallest of these calls take a few
 # microseconds on the GPU, so the checks are written to cost less than that.
 
+_torch_module = None                   # torch, once a call has needed it
+
 ACTS = ("none", "relu", "tanh", "sigmoid", "silu", "gelu")
 PACK_BLOCK = 128
 _ACT_CODES = {name: i for i, name in enumerate(ACTS)}
@@ -448,23 +452,22 @@ def _act_code(act: str) -> int:
 
 def _gpu(t, torch, name: str) -> int:
     """The number of the GPU that the tensor lies on."""
-    if not isinstance(t, torch.Tensor):
-        raise TypeError(f"{name} must be a GPU tensor")
-    device = t.get_device()
-    if device < 0:
-        raise TypeError(f"{name} must be a GPU tensor")
-    return device
+    if isinstance(t, torch.Tensor):
+        device = t.get_device()
+        if device >= 0:
+            return device
+    raise TypeError(f"{name} must be a GPU tensor")
 
 
 def _dense(t, torch, name: str):
     """(dtype code, rows, cols, stride) of a dense 2-D matrix with contiguous rows."""
-    dtype = t.dtype
-    code = 0 if dtype == torch.float32 else 1 if dtype == torch.bfloat16 else 2 if dtype == torch.float16 else -1
+    dtype, shape = t.dtype, t.shape
+    code = 1 if dtype == torch.bfloat16 else 0 if dtype == torch.float32 else 2 if dtype == torch.float16 else -1
     if code < 0:
         raise TypeError(f"{name} must be a float32, bfloat16 or float16 tensor, got {dtype}")
-    if t.dim() != 2:
+    if len(shape) != 2:
         raise ValueError(f"{name} must be 2-D with contiguous rows")
-    rows, cols = t.shape
+    rows, cols = shape
     stride, one = t.stride()
     if cols < 1 or (one != 1 and cols > 1):
         raise ValueError(f"{name} must be 2-D with contiguous rows")
@@ -473,20 +476,20 @@ def _dense(t, torch, name: str):
 
 def _packed(codes, scales, rows: int, cols: int, torch, name: str):
     """(code_stride, scale_stride) of the packed matrix `name` that must hold rows x cols values."""
-    nb = -(-cols // PACK_BLOCK)
-    strides = []
-    for t, least, of, what in ((codes, nb * PACK_BLOCK, PACK_BLOCK, "codes"), (scales, nb, 4, "scales")):
-        if t.dtype != torch.uint8:
-            raise TypeError(f"{name}{what} must have dtype torch.uint8, got {t.dtype}")
-        if t.dim() != 2:
-            raise ValueError(f"{name}{what} must be 2-D with contiguous rows")
-        have, width = t.shape
-        stride, one = t.stride()
-        # the last row, too, is read to its multiple
-        if have != rows or width < least or width % of or one != 1:
-            raise ValueError(f"{name}{what} must have {rows} contiguous rows of at least {least} bytes, a multiple of {of}")
-        strides.append(stride if rows > 1 else width)
-    return strides
+    u8, c_shape, s_shape = torch.uint8, codes.shape, scales.shape
+    if codes.dtype != u8 or scales.dtype != u8:
+        raise TypeError(f"{name}codes and {name}scales must have dtype torch.uint8, got {codes.dtype} and {scales.dtype}")
+    if len(c_shape) != 2 or len(s_shape) != 2:
+        raise ValueError(f"{name}codes and {name}scales must be 2-D with contiguous rows")
+    (c_rows, c_width), (s_rows, s_width) = c_shape, s_shape
+    (c_stride, c_one), (s_stride, s_one) = codes.stride(), scales.stride()
+    nb = (cols + PACK_BLOCK - 1) // PACK_BLOCK
+    # (the last row, too, is read to its multiple)
+    if c_rows != rows or c_width < nb * PACK_BLOCK or c_width % PACK_BLOCK or c_one != 1:
+        raise ValueError(f"{name}codes must have {rows} contiguous rows of at least {nb * PACK_BLOCK} bytes, a multiple of {PACK_BLOCK}")
+    if s_rows != rows or s_width < nb or s_width % 4 or s_one != 1:
+        raise ValueError(f"{name}scales must have {rows} contiguous rows of at least {nb} bytes, a multiple of 4")
+    return (c_stride, s_stride) if rows > 1 else (c_width, s_width)
 
 
 def _workspace(ws, torch) -> int:
@@ -495,43 +498,42 @@ def _workspace(ws, torch) -> int:
     return ws.numel()
 
 
-def _run(name: str, torch, devices, *args) -> None:
-    """Calls an entry point on the tensors' GPU, with its current stream as the last argument."""
+def _run(f, torch, devices, *args) -> None:
+    """Calls the entry point `f` on the tensors' GPU, with its current stream as the last argument."""
     device = devices[0]
     for other in devices:
         if other != device:
-            raise ValueError(f"{name}: tensors lie on several GPUs: {sorted(set(devices))}")
-    f = getattr(_lib or load(), name)
+            raise ValueError(f"{f.__name__}: tensors lie on several GPUs: {sorted(set(devices))}")
     stream = torch._C._cuda_getCurrentRawStream(device)
-    if device == torch.cuda.current_device():
+    if device == torch._C._cuda_getDevice():
         rc = f(*args, stream)
     else:
         with torch.cuda.device(device):
             rc = f(*args, stream)
     if rc:
-        raise GtopkError(rc, name)
+        raise GtopkError(rc, f.__name__)
 
 
 def alloc_packed(rows: int, cols: int, device="cuda"):
     """(codes, scales) of a packed matrix of rows x cols values, for the pack calls to fill."""
-    torch = _torch()
+    torch = _torch_module or _torch()
     nb = -(-cols // PACK_BLOCK)
     return (torch.empty((rows, nb * PACK_BLOCK), dtype=torch.uint8, device=device),
             torch.empty((rows, -(-nb // 4) * 4), dtype=torch.uint8, device=device))
 
 
 def gtopk_pack_rows(x, codes, scales) -> None:
-    torch = _torch()
+    torch = _torch_module or _torch()
     devices = (_gpu(x, torch, "x"), _gpu(codes, torch, "codes"), _gpu(scales, torch, "scales"))
     dtype, rows, cols, stride = _dense(x, torch, "x")
     code_stride, scale_stride = _packed(codes, scales, rows, cols, torch, "")
-    _run("gtopk_pack_rows", torch, devices, x.data_ptr(), dtype, rows, cols, stride, codes.data_ptr(), code_stride,
+    _run((_lib or load()).gtopk_pack_rows, torch, devices, x.data_ptr(), dtype, rows, cols, stride, codes.data_ptr(), code_stride,
          scales.data_ptr(), scale_stride)
 
 
 def gtopk_pack_tiles(x, codes=None, scales=None, codes_t=None, scales_t=None) -> None:
     """Either pair may be None, not both."""
-    torch = _torch()
+    torch = _torch_module or _torch()
     devices = [_gpu(x, torch, "x")]
     dtype, rows, cols, stride = _dense(x, torch, "x")
     args = []
@@ -544,21 +546,21 @@ def gtopk_pack_tiles(x, codes=None, scales=None, codes_t=None, scales_t=None) ->
         devices += (_gpu(c, torch, name + "codes"), _gpu(s, torch, name + "scales"))
         code_stride, scale_stride = _packed(c, s, *shape, torch, name) if rows else (0, 0)
         args += (c.data_ptr(), code_stride, s.data_ptr(), scale_stride)
-    _run("gtopk_pack_tiles", torch, devices, x.data_ptr(), dtype, rows, cols, stride, *args)
+    _run((_lib or load()).gtopk_pack_tiles, torch, devices, x.data_ptr(), dtype, rows, cols, stride, *args)
 
 
 def gtopk_unpack(codes, scales, act: str, out) -> None:
-    torch = _torch()
+    torch = _torch_module or _torch()
     devices = (_gpu(codes, torch, "codes"), _gpu(scales, torch, "scales"), _gpu(out, torch, "out"))
     dtype, rows, cols, stride = _dense(out, torch, "out")
     code_stride, scale_stride = _packed(codes, scales, rows, cols, torch, "")
-    _run("gtopk_unpack", torch, devices, codes.data_ptr(), code_stride, scales.data_ptr(), scale_stride, rows, cols,
+    _run((_lib or load()).gtopk_unpack, torch, devices, codes.data_ptr(), code_stride, scales.data_ptr(), scale_stride, rows, cols,
          _act_code(act), out.data_ptr(), dtype, stride)
 
 
 def gtopk_activation_grad(codes, scales, act: str, dy, dx) -> None:
     """dx may be dy."""
-    torch = _torch()
+    torch = _torch_module or _torch()
     devices = (_gpu(codes, torch, "codes"), _gpu(scales, torch, "scales"), _gpu(dy, torch, "dy"), _gpu(dx, torch, "dx"))
     dtype, rows, cols, dy_stride = _dense(dy, torch, "dy")
     dx_dtype, dx_rows, dx_cols, dx_stride = _dense(dx, torch, "dx")
@@ -567,7 +569,7 @@ def gtopk_activation_grad(codes, scales, act: str, dy, dx) -> None:
     if dx_dtype != dtype:
         raise TypeError("dy and dx must have the same dtype")
     code_stride, scale_stride = _packed(codes, scales, rows, cols, torch, "")
-    _run("gtopk_activation_grad", torch, devices, codes.data_ptr(), code_stride, scales.data_ptr(), scale_stride, rows, cols,
+    _run((_lib or load()).gtopk_activation_grad, torch, devices, codes.data_ptr(), code_stride, scales.data_ptr(), scale_stride, rows, cols,
          _act_code(act), dy.data_ptr(), dy_stride, dx.data_ptr(), dx_stride, dtype)
 
 
@@ -576,7 +578,7 @@ def gtopk_product_workspace_bytes(M: int, N: int, K: int) -> int:
 
 
 def alloc_product_workspace(M: int, N: int, K: int, device="cuda"):
-    torch = _torch()
+    torch = _torch_module or _torch()
     n = gtopk_product_workspace_bytes(M, N, K)
     if n == 0:
         raise GtopkError(GTOPK_EINVAL, "gtopk_product_workspace_bytes")
@@ -585,7 +587,7 @@ def alloc_product_workspace(M: int, N: int, K: int, device="cuda"):
 
 def gtopk_scaled_product(a_codes, a_scales, b_codes, b_scales, K: int, out, ws) -> None:
     """out [M][N] = A B^T for packed A (M x K) and B (N x K)."""
-    torch = _torch()
+    torch = _torch_module or _torch()
     devices = (_gpu(a_codes, torch, "a_codes"), _gpu(a_scales, torch, "a_scales"), _gpu(b_codes, torch, "b_codes"),
                _gpu(b_scales, torch, "b_scales"), _gpu(out, torch, "out"), _gpu(ws, torch, "ws"))
     if K < 1:
@@ -593,7 +595,7 @@ def gtopk_scaled_product(a_codes, a_scales, b_codes, b_scales, K: int, out, ws) 
     dtype, M, N, stride = _dense(out, torch, "out")
     a_stride, as_stride = _packed(a_codes, a_scales, M, K, torch, "a_")
     b_stride, bs_stride = _packed(b_codes, b_scales, N, K, torch, "b_")
-    _run("gtopk_scaled_product", torch, devices, a_codes.data_ptr(), a_stride, a_scales.data_ptr(), as_stride,
+    _run((_lib or load()).gtopk_scaled_product, torch, devices, a_codes.data_ptr(), a_stride, a_scales.data_ptr(), as_stride,
          b_codes.data_ptr(), b_stride, b_scales.data_ptr(), bs_stride, M, N, K, out.data_ptr(), dtype, stride,
          ws.data_ptr(), _workspace(ws, torch))
 
@@ -603,7 +605,7 @@ def gtopk_weight_grad_workspace_bytes(rows: int, P: int, N: int, K: int) -> int:
 
 
 def alloc_weight_grad_workspace(rows: int, P: int, N: int, K: int, device="cuda"):
-    torch = _torch()
+    torch = _torch_module or _torch()
     n = gtopk_weight_grad_workspace_bytes(rows, P, N, K)
     if n == 0:
         raise GtopkError(GTOPK_EINVAL, "gtopk_weight_grad_workspace_bytes")
@@ -613,7 +615,7 @@ def alloc_weight_grad_workspace(rows: int, P: int, N: int, K: int, device="cuda"
 def gtopk_weight_grad(dy, codes, scales, row_begin, grad, accumulate: bool, ws) -> None:
     """grad: float32 [P][N][K], for example grads[:, at:at + N*K].unflatten(1, (N, K)) of the workers' gradient rows;
     row_begin: int32 [P + 1] on the GPU, or None for equal shares."""
-    torch = _torch()
+    torch = _torch_module or _torch()
     devices = [_gpu(dy, torch, "dy"), _gpu(codes, torch, "codes"), _gpu(scales, torch, "scales"), _gpu(grad, torch, "grad"),
                _gpu(ws, torch, "ws")]
     dtype, rows, N, dy_stride = _dense(dy, torch, "dy")
@@ -634,6 +636,6 @@ def gtopk_weight_grad(dy, codes, scales, row_begin, grad, accumulate: bool, ws) 
             raise ValueError("row_begin must hold P + 1 entries")
         begin = row_begin.data_ptr()
     code_stride, scale_stride = _packed(codes, scales, rows, K, torch, "")
-    _run("gtopk_weight_grad", torch, devices, dy.data_ptr(), dtype, dy_stride, codes.data_ptr(), code_stride,
+    _run((_lib or load()).gtopk_weight_grad, torch, devices, dy.data_ptr(), dtype, dy_stride, codes.data_ptr(), code_stride,
          scales.data_ptr(), scale_stride, rows, begin, P, N, K, grad.data_ptr(), p_stride if P > 1 else N * K,
          1 if accumulate else 0, ws.data_ptr(), _workspace(ws, torch))
