@@ -27,6 +27,7 @@ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline uint32_t grid_for(uint64_t jobs) { return (uint32_t)(jobs < kMaxBlocks ? jobs : kMaxBlocks); }
 inline int launch_status() { return hipGetLastError() == hipSuccess ? GTOPK_OK : GTOPK_EHIP; }
 inline size_t value_bytes(int32_t dtype) { return dtype == GTOPK_F32 ? 4 : 2; }
+inline int value_parts(int32_t dtype) { return dtype == GTOPK_BF16 ? 1 : dtype == GTOPK_F16 ? 2 : 3; }
 inline bool dtype_ok(int32_t dtype) { return dtype == GTOPK_F32 || dtype == GTOPK_BF16 || dtype == GTOPK_F16; }
 inline bool act_ok(int32_t act) { return act >= GTOPK_ACT_NONE && act <= GTOPK_ACT_GELU; }
 inline bool side_ok(int64_t n, int64_t least) { return n >= least && n <= kMaxSide; }
@@ -104,9 +105,10 @@ struct GradPlan {
     int64_t part_stride;                // values of one worker's share
     uint64_t jobs;
 };
-constexpr uint64_t kMaxJobs = 0x7FFFFFFF;
+constexpr uint64_t kMaxJobs = 0x3FFFFFFF;
 constexpr int64_t kGradShareRows = 256, kGradShareRowsBig = 512;    // rows of a share, at least
-constexpr uint32_t kGradBand = 4, kGradBandBig = 8;                 // tiles across in a band (tile_at)
+constexpr uint32_t kGradBandBig = 8;                                // large tiles across in a band (tile_at); small ones: whole rows
+constexpr int64_t kGradLinesK = 512, kGradLinesRows = 256;         // (rows times the parts of a dY value)
 GradPlan grad_plan_of(bool big, int64_t rows, int32_t P, int64_t N, int64_t K) {
     GradPlan g;
     const int64_t side = big ? 256 : 128;
@@ -289,22 +291,27 @@ int gtopk_weight_grad(const void* dy, int32_t dtype, int64_t dy_stride, const ui
     const bool split = g.splits > 1;
     float* const to = split ? (float*)ws : grad;
     const int64_t to_stride = split ? g.part_stride : grad_stride, split_stride = split ? g.part_stride * P : 0;
-    // Where a row's tiles end inside memory lines, whole rows of tiles run side by side, so that the two writes of a line meet
-    // in L2 (4096 x 9217: 3.4 TB/s in bands of 4 tiles, 5.0 in whole rows); otherwise bands are the better (4096 x 4096: 5.5 and 4.8)
-    const bool whole_lines = K % 32 == 0 && to_stride % 32 == 0 && aligned(to, 128);
-    const uint32_t band = !whole_lines ? g.tiles_k : g.big ? kGradBandBig : kGradBand;
+    // Rows of whole memory lines (K a multiple of 32): tiles that begin where lines do, also in a row that does not, write past
+    // the caches (LINES), the last of up to 31 more columns; where writing bounds the call, and from kGradLinesK on, where the
+    // extra column of tiles is a small part.  (TB/s, 64 rows of every worker, without / with: 4096 x 9216 5.2 / 6.1; 1000 x 4096 4.4
+    // / 5.9; 2048 x 2048 4.3 / 6.3; the shares of 1501 rows by seven random cuts, 1000 x 4096 in fp32: 79 us without, 110 with.)
+    const bool aligned_rows = K % 32 == 0 && to_stride % 32 == 0 && aligned(to, 128);
+    const bool lines = !g.big && (aligned_rows || (K % 32 == 0 && K >= kGradLinesK && !split && rows / P * (int64_t)value_parts(dtype) <= kGradLinesRows));
+    const uint32_t tiles_k = lines && !aligned_rows ? (uint32_t)ceil_div(K + 31, 128) : g.tiles_k;
+    const uint32_t jobs = g.tiles_n * tiles_k * (uint32_t)P * g.splits, band = g.big ? kGradBandBig : tiles_k;
     hipStream_t st = (hipStream_t)stream;
     by_type(dtype, [&](auto d) {
         using D = decltype(d);
         auto launch = [&](auto kernel, int threads) {
-            hipLaunchKernelGGL(kernel, dim3(grid_for(g.jobs)), dim3(threads), 0, st, (const typename D::T*)dy, dy_stride, codes, code_stride,
+            hipLaunchKernelGGL(kernel, dim3(grid_for(jobs)), dim3(threads), 0, st, (const typename D::T*)dy, dy_stride, codes, code_stride,
                                scales, scale_stride, rows, row_begin, (uint32_t)P, N, K, to, to_stride, split ? 0 : accumulate != 0,
-                               g.splits, split_stride, g.tiles_n, g.tiles_k, band, (uint32_t)g.jobs);
+                               g.splits, split_stride, g.tiles_n, tiles_k, band, jobs);
         };
         if constexpr (Parts<D>::n == 1) {
-            if (g.big) return launch(k_weight_grad<D, 256, 256, 128, 64>, 512);
+            if (g.big) return launch(k_weight_grad<D, 256, 256, 128, 64, false>, 512);
         }
-        launch(k_weight_grad<D, 128, 128, 64, 64>, 256);
+        if (lines) launch(k_weight_grad<D, 128, 128, 64, 64, true>, 256);
+        else launch(k_weight_grad<D, 128, 128, 64, 64, false>, 256);
     });
     if (split) {
         const int64_t blocks = ceil_div(N * K, 4 * kPackThreads);

@@ -68,6 +68,11 @@ __device__ __forceinline__ void decode16(uint32x4 c, float scale, uint32x4& lo, 
     }
 }
 
+// two values (a word): the first n from block 0, the rest from block 1
+__device__ __forceinline__ uint32_t two_blocks(uint32_t in0, uint32_t in1, int n) {
+    return n >= 2 ? in0 : n <= 0 ? in1 : (in0 & 0xFFFFu) | (in1 & 0xFFFF0000u);
+}
+
 constexpr int kGradRows = 32;               // rows of dY and X in one step
 
 // A block computes BN x BK values of one worker (rows of dW from dY's columns, columns from X's) over all of its rows,
@@ -77,13 +82,17 @@ constexpr int kGradRows = 32;               // rows of dY and X in one step
 // matrix instruction wants.  (Which 8 of the 32 rows a lane holds is free as long as both operands agree: the
 // four groups of 16 lanes take rows 4 g .. 4 g + 3 and 16 + 4 g .. , so that with 8 words between the rows'
 // banks 16 lanes' pieces of 32 bytes fall on all of them.)
-// Tiles of 128 x 128 with four waves, two blocks per compute unit: where workers have few rows, writing dW bounds the call (16
-// workers, 64 rows each, 4096 x 9216: 2.4 GB in 440 us = 5.6 TB/s).  Tiles of 256 x 256 with eight waves for long sums in
+// Tiles of 128 x 128 with four waves: where workers have few rows, writing dW bounds the call, and three blocks per compute unit
+// overlap one's stores with another's loads (16 workers, 64 rows each, 4096 x 9216: 2.4 GB, nearly all of it written, in 409 us =
+// 6.0 TB/s; a fill writes 6.9).  Tiles of 256 x 256 with eight waves for long sums in
 // bf16: half the LDS traffic and loads per product (16384 rows, 4096 x 4096: 463 us = 1.19 PFLOP/s, with tiles of 128 677 us);
 // there (kAhead) the next rows are staged while the matrix instructions run, also behind the last step, which would cost
 // a quarter of the call where workers have two steps.
-template <class D, int BN, int BK, int WN, int WK>
-__global__ __launch_bounds__((BN / WN) * (BK / WK) * kWave, BN * BK > 128 * 128 ? 1 : 2) void k_weight_grad(
+// LINES: K is a multiple of 32, so dW's rows all begin at the same place in a memory line, but a layer may lie anywhere in its
+// worker's row.  Tiles that begin where lines do have whole lines to write, which go past the caches; a line written in two pieces
+// by two blocks costs more than twice (4096 x 9216 from an odd place: 484 us without LINES).
+template <class D, int BN, int BK, int WN, int WK, bool LINES>
+__global__ __launch_bounds__((BN / WN) * (BK / WK) * kWave, BN * BK > 128 * 128 ? 1 : Parts<D>::n == 1 ? 3 : 2) void k_weight_grad(
         const typename D::T* __restrict__ dy, int64_t dy_stride, const uint8_t* __restrict__ codes, int64_t code_stride,
         const uint8_t* __restrict__ scales, int64_t scale_stride, int64_t rows, const int32_t* __restrict__ begin, uint32_t P,
         int64_t N, int64_t K, float* __restrict__ grad, int64_t grad_stride, int accumulate, uint32_t splits, int64_t split_stride,
@@ -114,7 +123,9 @@ __global__ __launch_bounds__((BN / WN) * (BK / WK) * kWave, BN * BK > 128 * 128 
         tile_at(job % tiles, tiles_k, tiles_n, band, tile_k, tile_n);
         job /= tiles;
         const uint32_t split = job % splits, w = job / splits;
-        const int64_t n0 = (int64_t)tile_n * BN, k0 = (int64_t)tile_k * BK;
+        float* const to = grad + w * grad_stride + split * split_stride;
+        // (LINES: the tile's columns start where a memory line of dW's rows does, up to 31 columns before a block of 128)
+        const int64_t n0 = (int64_t)tile_n * BN, k0 = (int64_t)tile_k * BK - (LINES ? (int64_t)((uintptr_t)to / 4 % 32) : 0);
         int64_t first, last;
         rows_of_worker(begin, rows, P, w, first, last);
         if (splits > 1) {                  // shares of whole steps
@@ -128,10 +139,15 @@ __global__ __launch_bounds__((BN / WN) * (BK / WK) * kWave, BN * BK > 128 * 128 
         const uint32_t n_at = threadIdx.x % (BN / 8) * 8, d_row = threadIdx.x / (BN / 8);
         const uint32_t k_at = threadIdx.x % (BK / 16) * 16, x_row = threadIdx.x / (BK / 16);
         const int64_t n_left = N - (n0 + n_at);
-        const bool k_in = k0 + k_at < (K + kPackBlock - 1) / kPackBlock * kPackBlock;
+        const int64_t k_first = k0 + k_at, k_end = (K + kPackBlock - 1) / kPackBlock * kPackBlock;
+        const bool k_in = LINES ? k_first > -16 && k_first < k_end : k_first < k_end, k_whole = !LINES || (k_first >= 0 && k_first + 16 <= k_end);
+        // (LINES: 16 codes may lie in two blocks of 128, the first `k_cut` in the first one)
+        const int64_t block0 = LINES && k_first < 0 ? 0 : k_first / kPackBlock;
+        const uint32_t block1 = !LINES || k_first + 15 >= k_end ? 0u : (uint32_t)((k_first + 15) / kPackBlock - block0);
+        const int k_cut = block1 ? (int)((block0 + 1) * kPackBlock - k_first) : 16;
         const typename D::T* d_from = dy + (first + d_row) * dy_stride + n0 + n_at;
-        const uint8_t* x_from = codes + (first + x_row) * code_stride + k0 + k_at;
-        const uint8_t* s_from = scales + (first + x_row) * scale_stride + (k0 + k_at) / kPackBlock;
+        const uint8_t* x_from = codes + (first + x_row) * code_stride + k_first;
+        const uint8_t* s_from = scales + (first + x_row) * scale_stride + block0;
         int32_t left = (int32_t)(last - first);    // rows that have not been loaded
         // two steps' rows on their way, as they lie in memory: taken apart when they are staged
         Eight<D> d_next[2][kLoadsD];
@@ -154,8 +170,17 @@ __global__ __launch_bounds__((BN / WN) * (BK / WK) * kWave, BN * BK > 128 * 128 
                 x_next[set][i] = uint32x4{0u, 0u, 0u, 0u};
                 s_next[set][i] = 127u;
                 if ((int)x_row + i * (kThreads * 16 / BK) < left && k_in) {
-                    x_next[set][i] = *reinterpret_cast<const uint32x4*>(x_from + i * (kThreads * 16 / BK) * code_stride);
-                    s_next[set][i] = s_from[i * (kThreads * 16 / BK) * scale_stride];
+                    const uint8_t* p = x_from + i * (kThreads * 16 / BK) * code_stride;
+                    const uint8_t* q = s_from + i * (kThreads * 16 / BK) * scale_stride;
+                    if (k_whole) {
+                        struct __attribute__((packed)) Loose { uint32x4 v; };
+                        x_next[set][i] = LINES ? reinterpret_cast<const Loose*>(p)->v : *reinterpret_cast<const uint32x4*>(p);
+                    } else {               // at a row's ends: what lies outside the row is not read
+#pragma unroll
+                        for (int e = 0; e < 16; ++e)
+                            if (k_first + e >= 0 && k_first + e < k_end) x_next[set][i][e / 4] |= (uint32_t)p[e] << (e % 4 * 8);
+                    }
+                    s_next[set][i] = LINES ? q[0] | (uint32_t)q[block1] << 8 : q[0];
                 }
             }
             d_from += kGradRows * dy_stride;
@@ -175,7 +200,16 @@ __global__ __launch_bounds__((BN / WN) * (BK / WK) * kWave, BN * BK > 128 * 128 
 #pragma unroll
             for (int i = 0; i < kLoadsX; ++i) {
                 uint32x4 lo, hi;
-                decode16(x_next[set][i], scale_value(s_next[set][i]), lo, hi);
+                decode16(x_next[set][i], scale_value(LINES ? s_next[set][i] & 255u : s_next[set][i]), lo, hi);
+                if (LINES && k_cut < 16) {
+                    uint32x4 lo1, hi1;
+                    decode16(x_next[set][i], scale_value(s_next[set][i] >> 8), lo1, hi1);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        lo[e] = two_blocks(lo[e], lo1[e], k_cut - 2 * e);
+                        hi[e] = two_blocks(hi[e], hi1[e], k_cut - 8 - 2 * e);
+                    }
+                }
                 uint32x4* to = reinterpret_cast<uint32x4*>(s_x + (buf * kGradRows + x_row + i * (kThreads * 16 / BK)) * kPitchX + k_at);
                 to[0] = lo;
                 to[1] = hi;
@@ -231,7 +265,6 @@ __global__ __launch_bounds__((BN / WN) * (BK / WK) * kWave, BN * BK > 128 * 128 
         if (step < steps) step_at(step, 0);
         // A lane holds four consecutive columns of a row of dW, and a wave's store would write pieces of 64 bytes of 16 rows; by way
         // of LDS (each wave its own part, 16 rows at a time) it writes 4 WK bytes of a row at a stretch.
-        float* const to = grad + w * grad_stride + split * split_stride;
         float* const s_out = reinterpret_cast<float*>(s_rows) + wave * 16 * kPitchOut;
         constexpr int kAcross = WK / 4;        // lanes per row
 #pragma unroll
@@ -244,8 +277,20 @@ __global__ __launch_bounds__((BN / WN) * (BK / WK) * kWave, BN * BK > 128 * 128 
                 const int row = r + lane / kAcross, col = lane % kAcross * 4;
                 floatx4 v = *reinterpret_cast<const floatx4*>(s_out + row * kPitchOut + col);
                 const int64_t n = n0 + wn + j * 16 + row, k = k0 + wk + col;
-                if (n < N && k < K) {
-                    float* p = to + n * K + k;
+                if (n >= N || k >= K) continue;
+                float* p = to + n * K + k;
+                if constexpr (LINES) {
+                    const int64_t line = k - col % 32;
+                    if (line >= 0 && line + 32 <= K) {         // a whole line: past the caches
+                        floatx4* const q = reinterpret_cast<floatx4*>(p);
+                        if (accumulate) v = *q + v;
+                        __builtin_nontemporal_store(v, q);
+                    } else {                   // the lines that two rows share
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (k + e >= 0 && k + e < K) p[e] = accumulate ? p[e] + v[e] : v[e];
+                    }
+                } else {
                     if (accumulate) {
 #pragma unroll
                         for (int e = 0; e < 4; ++e)

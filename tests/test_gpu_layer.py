@@ -380,6 +380,7 @@ GRADS = [(1, 1, 1, 1, "even"), (1, 1, 5, 300, "even"), (4, 4, 3, 2, "even"), (2,
          (3, 33, 17, 40, "ragged"), (4, 100, 64, 128, "loose"), (2, 500, 128, 128, "even"), (1, 2000, 100, 260, "even"),
          (5, 77, 257, 385, "ragged"), (1, 9000, 33, 65, "even"), (8, 1501, 100, 131, "ragged"), (16, 1024, 256, 130, "even"),
          (1, 0, 20, 30, "even"), (6, 3, 9, 140, "loose"), (32, 32 * 40, 40, 200, "even"),
+         (3, 70, 40, 512, "ragged"), (2, 300, 130, 1024, "even"), (4, 64, 33, 544, "even"), (1, 33, 20, 640, "even"),
          (2, 6000, 1000, 1100, "ragged"), (3, 4700, 1025, 770, "loose"), (1, 9001, 1030, 900, "even")]
 
 
@@ -412,6 +413,34 @@ def test_weight_grad_of_integers_is_exact(P, rows, N, K, kind, dtype):
     B.gtopk_weight_grad(d, c, s, plan, grad, True, ws)
     assert torch.equal(grad.cpu(), 2 * w32)
     assert bool((grads[:, :behind] == 7.0).all()) and bool((grads[:, behind + N * K:] == 7.0).all())
+
+
+@pytest.mark.parametrize("behind,gap", [(0, 0), (32, 32), (1, 0), (31, 1), (7, 25), (16, 8), (30, 3), (100, 28)])
+@pytest.mark.parametrize("K", [512, 608, 1152, 96])
+def test_weight_grad_wherever_rows_begin(behind, gap, K):
+    """dW anywhere in the workers' rows, in front of and behind other layers: tiles follow memory lines, sums do not."""
+    import torch
+    from paper_1901_04359_amd import binding as B
+    P, T, N = 3, 45, 37
+    codes, scales = int_packed(P * T, K, 31)
+    dy = np.random.default_rng([behind, K]).integers(-8, 9, (P * T, N)).astype(np.float64)
+    want = torch.from_numpy(ref.weight_grad(dy, ref.values(codes, scales, K), [0, T, 2 * T, 3 * T])).float()
+    base = torch.full((64 + P * (behind + N * K + gap) + 64,), 7.0, device="cuda")
+    assert base.data_ptr() % 128 == 0
+    grads = base[64:-64].view(P, behind + N * K + gap)
+    grad = grads[:, behind:behind + N * K].unflatten(1, (N, K))
+    ws = B.alloc_weight_grad_workspace(P * T, P, N, K)
+    c, s = packed_on_gpu(codes, scales)
+    say(f"layer: weight_grad behind {behind} gap {gap} K {K}")
+    for dtype in TYPES:
+        d = on_gpu(dy, torch_type(dtype))
+        B.gtopk_weight_grad(d, c, s, None, grad, False, ws)
+        assert torch.equal(grad.cpu(), want)
+        B.gtopk_weight_grad(d, c, s, None, grad, True, ws)
+        assert torch.equal(grad.cpu(), 2 * want)
+        rest = base.clone()
+        rest[64:-64].view(P, -1)[:, behind:behind + N * K] = 7.0
+        assert bool((rest == 7.0).all())
 
 
 @pytest.mark.parametrize("P,rows,N,K,kind", [(4, 300, 70, 200, "ragged"), (1, 5000, 130, 140, "even"), (16, 16, 64, 300, "even")])
