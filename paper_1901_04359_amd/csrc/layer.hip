@@ -107,7 +107,9 @@ struct GradPlan {
 };
 constexpr uint64_t kMaxJobs = 0x3FFFFFFF;
 constexpr int64_t kGradShareRows = 256, kGradShareRowsBig = 512;    // rows of a share, at least
-constexpr uint32_t kGradBandBig = 8;                                // large tiles across in a band (tile_at); small ones: whole rows
+// Tiles across in a band (tile_at) where products bound the call and L2 has to hold dY and X (in us, 4 / 8 / whole rows: 8192 rows, 4096 x
+// 4096 in fp32 803 / 812 / 872).  Whole rows of tiles where writing does, or where two tiles write one memory line.
+constexpr uint32_t kGradBand = 4;
 constexpr int64_t kGradLinesK = 512, kGradLinesRows = 256;         // (rows times the parts of a dY value)
 GradPlan grad_plan_of(bool big, int64_t rows, int32_t P, int64_t N, int64_t K) {
     GradPlan g;
@@ -296,9 +298,10 @@ int gtopk_weight_grad(const void* dy, int32_t dtype, int64_t dy_stride, const ui
     // extra column of tiles is a small part.  (TB/s, 64 rows of every worker, without / with: 4096 x 9216 5.2 / 6.1; 1000 x 4096 4.4
     // / 5.9; 2048 x 2048 4.3 / 6.3; the shares of 1501 rows by seven random cuts, 1000 x 4096 in fp32: 79 us without, 110 with.)
     const bool aligned_rows = K % 32 == 0 && to_stride % 32 == 0 && aligned(to, 128);
-    const bool lines = !g.big && (aligned_rows || (K % 32 == 0 && K >= kGradLinesK && !split && rows / P * (int64_t)value_parts(dtype) <= kGradLinesRows));
+    const bool writes = rows / P * (int64_t)value_parts(dtype) <= kGradLinesRows;
+    const bool lines = !g.big && writes && (aligned_rows || (K % 32 == 0 && K >= kGradLinesK && !split));
     const uint32_t tiles_k = lines && !aligned_rows ? (uint32_t)ceil_div(K + 31, 128) : g.tiles_k;
-    const uint32_t jobs = g.tiles_n * tiles_k * (uint32_t)P * g.splits, band = g.big ? kGradBandBig : tiles_k;
+    const uint32_t jobs = g.tiles_n * tiles_k * (uint32_t)P * g.splits, band = writes || !aligned_rows ? tiles_k : kGradBand;
     hipStream_t st = (hipStream_t)stream;
     by_type(dtype, [&](auto d) {
         using D = decltype(d);
