@@ -100,7 +100,7 @@ ProductPlan product_plan(int64_t M, int64_t N, int64_t K) {
 // How the weight gradient's sums are cut: tiles of every worker's gradient, and where they are too few for the chip's 256 compute
 // units, shares of the rows, joined from the workspace.
 struct GradPlan {
-    bool big;                           // tiles of 256 x 256, one block per compute unit; else 128 x 128 and two
+    bool big;                           // tiles of 256 x 256, one block per compute unit; else 128 x 128, two or three
     uint32_t tiles_n, tiles_k, splits;
     int64_t part_stride;                // values of one worker's share
     uint64_t jobs;
@@ -128,7 +128,7 @@ GradPlan grad_plan_of(bool big, int64_t rows, int32_t P, int64_t N, int64_t K) {
 // Large tiles for sums of at least kGradShareRowsBig rows in bf16 (an fp16 or fp32 dY's two or three parts do not fit the
 // registers beside their sums), if they keep three quarters of the chip at work and add at most a quarter to
 // what the small ones compute behind the edges.  (In us, small / large: 16384 rows, 1024 x 1024 59 / 55; 4096 x 4096 677 / 463;
-// 64 rows of 16 workers, 4096 x 9216: 438 / 533.)
+// 64 rows of 16 workers, 4096 x 9216: 392 / 533.)
 GradPlan grad_plan(bool bf16, int64_t rows, int32_t P, int64_t N, int64_t K) {
     const GradPlan small = grad_plan_of(false, rows, P, N, K);
     if (!bf16 || rows / P < kGradShareRowsBig) return small;

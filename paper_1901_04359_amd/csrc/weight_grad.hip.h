@@ -11,7 +11,6 @@
 namespace gtopk {
 
 typedef short shortx4 __attribute__((ext_vector_type(4)));
-typedef short shortx8 __attribute__((ext_vector_type(8)));
 
 // first and last + 1 row of worker w; whatever begin[] holds, 0 <= first <= last <= rows
 __device__ __forceinline__ void rows_of_worker(const int32_t* begin, int64_t rows, uint32_t P, uint32_t w, int64_t& first, int64_t& last) {
@@ -103,7 +102,7 @@ __global__ __launch_bounds__((BN / WN) * (BK / WK) * kWave, BN * BK > 128 * 128 
     constexpr int kPitchD = BN + 16, kPitchX = BK + 16;                    // values; 8 words more than a multiple of the banks
     constexpr int kLoadsD = kGradRows * BN / 8 / kThreads, kLoadsX = kGradRows * BK / 16 / kThreads;
     static_assert(kLoadsD * kThreads * 8 == kGradRows * BN && kLoadsX * kThreads * 16 == kGradRows * BK, "whole loads");
-    static_assert(BK % kPackBlock == 0, "a lane's 16 codes lie in one block of 128");
+    static_assert(BK % kPackBlock == 0, "a lane's 16 codes lie in one block of 128, or in two with LINES");
     constexpr bool kAhead = BN * BK > 128 * 128;
     constexpr int kPitchOut = WK + 4;                                      // floats
     static_assert((BN / WN) * kWavesK * 16 * kPitchOut * 2 <= 2 * kGradRows * (kParts * kPitchD + kPitchX), "the result's rows fit the same memory");
@@ -114,9 +113,9 @@ __global__ __launch_bounds__((BN / WN) * (BK / WK) * kWave, BN * BK > 128 * 128 
     const uint32_t wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
     const uint32_t wn = (wave / kWavesK) * WN, wk = (wave % kWavesK) * WK;
     for (uint32_t id = blockIdx.x; id < jobs; id += gridDim.x) {
-        // Equal shares: an XCD gets whole workers, whose rows then lie in its L2 (32 workers, 64 rows each, 4096 x 4096: 384 us, spread
-        // out 455).  Uneven ones: every worker's tiles are spread over all XCDs (the shares of 1501 rows by seven random cuts,
-        // 1000 x 4096 in fp32: 76 us, by XCD 167).
+        // Equal shares: an XCD gets whole workers, whose rows then lie in its L2 (TB/s with 64 rows of every worker, whole / spread out:
+        // 4096 x 1024 5.9 / 5.5, 1000 x 4096 5.8 / 5.3, 4096 x 9217 4.9 / 4.6, larger ones alike).  Uneven ones: every worker's tiles are
+        // spread over all XCDs (the shares of 1501 rows by seven random cuts, 1000 x 4096 in fp32: 76 us, by XCD 167).
         const uint32_t tiles = tiles_n * tiles_k, spread = begin ? tiles * splits : jobs, at = id / spread * spread;
         uint32_t job = at + by_xcd(id - at, spread);
         uint32_t tile_n, tile_k;

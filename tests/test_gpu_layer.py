@@ -576,6 +576,38 @@ def test_offsets_past_32_bits():
     assert bool(((grad[0] - want).abs() <= 200 * 2.0 ** -22 * want.abs().max()).all())
 
 
+def test_more_rows_and_jobs_than_blocks_in_a_launch():
+    """Grids are capped: blocks walk the rows, and the workers' tiles, that are left."""
+    import torch
+    from paper_1901_04359_amd import binding as B
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(6)
+    rows, cols = 2_200_000, 9                                # 65535 blocks of 16 or 32 rows, and 100,000 rows more
+    for t in (torch.float32, torch.bfloat16):
+        x = torch.empty(rows, cols, device="cuda").normal_(generator=gen).to(t)
+        codes, scales = B.alloc_packed(rows, cols)
+        out = torch.zeros_like(x)
+        say(f"layer: {rows} rows of {cols}")
+        B.gtopk_pack_rows(x, codes, scales)
+        B.gtopk_unpack(codes, scales, "none", out)
+        assert bool(((out - x).float().abs() <= x.float().abs().amax(dim=1, keepdim=True) * 2.0 ** -4).all())
+        for at in (0, 1_048_500, 2_097_100, rows - 60):
+            want = ref.values(*ref.pack(x[at:at + 60].double().cpu().numpy()), cols)
+            assert np.array_equal(out[at:at + 60].double().cpu().numpy(), want)
+        B.gtopk_activation_grad(codes, scales, "relu", x, x)
+        assert torch.equal(x, torch.where(out > 0, x, torch.zeros_like(x)))
+        del x, out, codes, scales
+    P, K = 32768, 130 * 128                                  # 4.26 million tiles
+    x = torch.randint(-4, 5, (P, K), device="cuda", generator=gen, dtype=torch.int32).to(torch.bfloat16)
+    codes, scales = B.alloc_packed(P, K)
+    B.gtopk_pack_rows(x, codes, scales)
+    dy = torch.randint(-8, 9, (P, 1), device="cuda", generator=gen, dtype=torch.int32).to(torch.bfloat16)
+    grad = torch.empty(P, 1, K, device="cuda")
+    say("layer: weight_grad of 32768 workers")
+    B.gtopk_weight_grad(dy, codes, scales, None, grad, False, B.alloc_weight_grad_workspace(P, P, 1, K))
+    assert torch.equal(grad[:, 0], dy.float() * x.float())
+
+
 # ---- together, on streams, in graphs --------------------------------------------------
 
 class Layers:
