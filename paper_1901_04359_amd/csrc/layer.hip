@@ -73,7 +73,7 @@ PackGrid pack_grid(int64_t rows, int64_t cols, int32_t dtype, dim3* grid) {
 // How a product is computed: few rows of A without tiles, else tiles of 128 x 128, and where they are too few for the
 // chip's 256 compute units (two blocks each), shares of K, joined from the workspace.
 struct ProductPlan {
-    bool thin;
+    bool thin, large;                               // large: tiles of 256 x 256, one block per compute unit
     uint32_t tiles_m, tiles_n, share, shares;       // blocks of 128 per share
     int64_t stride;                                 // of a share's result
 };
@@ -89,6 +89,18 @@ ProductPlan product_plan(int64_t M, int64_t N, int64_t K) {
     g.tiles_m = (uint32_t)ceil_div(M, 128);
     g.tiles_n = (uint32_t)ceil_div(N, 128);
     g.stride = ceil_div(N, 4) * 4;
+    // A round of large tiles over the chip takes 1.67 times as long as one of small ones, two to a compute unit, and does twice as much (us,
+    // small / large: 8192^3 509 / 425; 4096^3 71 / 61; 8187 x 9216 x 4096 305 / 283, to fp32 538 / 491; 2048 x 4096 x 9216, half a round of large
+    // ones, 72 / 111).
+    const uint64_t tiles_large = (uint64_t)ceil_div(M, 256) * ceil_div(N, 256);
+    g.large = !g.thin && 5 * ((tiles_large + 255) / 256) < 3 * (((uint64_t)g.tiles_m * g.tiles_n + 511) / 512);
+    g.share = nb;
+    g.shares = 1;
+    if (g.large) {
+        g.tiles_m = (uint32_t)ceil_div(M, 256);
+        g.tiles_n = (uint32_t)ceil_div(N, 256);
+        return g;
+    }
     const uint64_t tiles = (uint64_t)g.tiles_m * g.tiles_n;
     uint64_t want = g.thin || tiles == 0 ? 1 : 512 / tiles;
     if (want > nb / kProductShare) want = nb / kProductShare;
@@ -252,6 +264,11 @@ int gtopk_scaled_product(const uint8_t* a_codes, int64_t a_code_stride, const ui
             const dim3 grid((uint32_t)ceil_div(N, 16)), block(kThinWaves * kWave);
             if (M <= 16) hipLaunchKernelGGL((k_product_thin<D, 1>), grid, block, 0, st, a, b, M, N, nb, to, out_stride);
             else hipLaunchKernelGGL((k_product_thin<D, 2>), grid, block, 0, st, a, b, M, N, nb, to, out_stride);
+            return;
+        }
+        if (g.large) {
+            hipLaunchKernelGGL((k_product<D, Exact<D>::value, 256, 256, 128, 64>), dim3(g.tiles_m * g.tiles_n), dim3(512), 0, st, a, b, M, N,
+                               nb, to, out_stride, g.tiles_m, g.tiles_n, nb);
             return;
         }
         if (g.shares == 1) {

@@ -47,19 +47,39 @@ __device__ __forceinline__ bf16x8 decode_bf16(int c0, int c1, float scale) {
     return __builtin_bit_cast(bf16x8, u);
 }
 
-// sum + one block of 128: B's row is the instruction's first operand, so a lane holds four consecutive columns of C.
-// The scales are byte BYTE of sb and sa.
-template <bool EXACT, int BYTE>
-__device__ __forceinline__ floatx4 multiply(intx8 vb, uint32_t sb, intx8 va, uint32_t sa, floatx4 sum) {
+// A row's 32 codes of one block of 128 as the matrix instruction takes them, with the row's scale (the lowest byte of `scale`)
+template <bool EXACT> struct Operand;
+template <> struct Operand<false> { intx8 codes; uint32_t scale; };
+template <> struct Operand<true> { bf16x8 values[4]; };
+template <bool EXACT>
+__device__ __forceinline__ Operand<EXACT> prepare(intx8 codes, uint32_t scale) {
+    Operand<EXACT> x;
     if constexpr (EXACT) {
-        const float fa = scale_value(sa >> (8 * BYTE) & 255u), fb = scale_value(sb >> (8 * BYTE) & 255u);
+        const float f = scale_value(scale & 255u);
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-            sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode_bf16(vb[2 * q], vb[2 * q + 1], fb), decode_bf16(va[2 * q], va[2 * q + 1], fa), sum, 0, 0, 0);
+        for (int q = 0; q < 4; ++q) x.values[q] = decode_bf16(codes[2 * q], codes[2 * q + 1], f);
+    } else {
+        x.codes = codes;
+        x.scale = scale;
+    }
+    return x;
+}
+// sum + one block of 128: B's row is the instruction's first operand, so a lane holds four consecutive columns of C
+template <bool EXACT>
+__device__ __forceinline__ floatx4 multiply(const Operand<EXACT>& b, const Operand<EXACT>& a, floatx4 sum) {
+    if constexpr (EXACT) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b.values[q], a.values[q], sum, 0, 0, 0);
         return sum;
     } else {
-        return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(vb, va, sum, 0, 0, BYTE, (int)sb, BYTE, (int)sa);
+        return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b.codes, a.codes, sum, 0, 0, 0, (int)b.scale, 0, (int)a.scale);
     }
+}
+// keeps the instructions that compute v in front of what follows
+__device__ __forceinline__ void pin(floatx4& v) {
+#ifdef __HIP_DEVICE_COMPILE__
+    asm volatile("" : "+v"(v));
+#endif
 }
 
 // A block computes BM x BN values with BM/WM x BN/WN waves of WM x WN each.  (Tiles of 128 x 128 with four waves, two blocks per
@@ -79,6 +99,7 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * kWave, 1) void k_product(
         uint32_t tiles_m, uint32_t tiles_n, uint32_t share) {
     constexpr int kWavesN = BN / WN, kWaves = (BM / WM) * kWavesN, kThreads = kWaves * kWave;
     constexpr int TM = WM / 16, TN = WN / 16;
+    constexpr bool kStream = TM > 4;         // A's rows are read 16 at a time, while the products of the ones before run
     constexpr int kScaleLoads = (BM + BN + kThreads - 1) / kThreads;
     constexpr int kStage = (BM + BN) * kPackBlock;
     constexpr int kLoads = kStage / 16 / kThreads;                 // 16-byte pieces per thread and stage
@@ -156,19 +177,42 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * kWave, 1) void k_product(
 #pragma unroll
             for (int j = 0; j < TN; ++j) sb[j] = from[BM + wn + j * 16 + in16];
         }
-        intx8 va[TM], vb[TN];
+        const uint32_t after = kb + 1 < nb ? kb + 1 : nb - 1, after_scales = kb + 1 < nb ? kb + 1 : kb & ~3u;
+        if constexpr (kStream) {
+            intx8 vb[TN];
 #pragma unroll
-        for (int j = 0; j < TN; ++j) vb[j] = operand(here, BM + wn + j * 16);
+            for (int j = 0; j < TN; ++j) vb[j] = operand(here, BM + wn + j * 16);
+            intx8 va = operand(here, wm);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int i = 0; i < TM; ++i) va[i] = operand(here, wm + i * 16);
-        __builtin_amdgcn_sched_barrier(0);         // the loads behind the reads that the first products wait for
-        fetch(kb + 1 < nb ? kb + 1 : nb - 1, free);
-        if (in4 == 3) fetch_scales(kb + 1 < nb ? kb + 1 : kb & ~3u, s_scales[(kb + 1) / 4 % 2]);
-        __builtin_amdgcn_sched_barrier(0);
+            for (int i = 0; i < TM; ++i) {
+                const intx8 va_next = i + 1 < TM ? operand(here, wm + (i + 1) * 16) : va;
+                if (i == 0) fetch(after, free);
+                if (in4 == 3 && i == TM - 1) fetch_scales(after_scales, s_scales[(kb + 1) / 4 % 2]);
+                const Operand<EXACT> xa = prepare<EXACT>(va, sa[i] >> (8 * in4));
 #pragma unroll
-        for (int i = 0; i < TM; ++i)
+                for (int j = 0; j < TN; ++j) sum[i][j] = multiply<EXACT>(prepare<EXACT>(vb[j], sb[j] >> (8 * in4)), xa, sum[i][j]);
+                va = va_next;
+                // these products here and not behind the next reads: the compiler moves them as far down as it may
 #pragma unroll
-            for (int j = 0; j < TN; ++j) sum[i][j] = multiply<EXACT, 0>(vb[j], sb[j] >> (8 * in4), va[i], sa[i] >> (8 * in4), sum[i][j]);
+                for (int j = 0; j < TN; ++j) pin(sum[i][j]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        } else {
+            intx8 va[TM], vb[TN];
+#pragma unroll
+            for (int j = 0; j < TN; ++j) vb[j] = operand(here, BM + wn + j * 16);
+#pragma unroll
+            for (int i = 0; i < TM; ++i) va[i] = operand(here, wm + i * 16);
+            __builtin_amdgcn_sched_barrier(0);         // the loads behind the reads that the first products wait for
+            fetch(after, free);
+            if (in4 == 3) fetch_scales(after_scales, s_scales[(kb + 1) / 4 % 2]);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j) sum[i][j] = multiply<EXACT>(prepare<EXACT>(vb[j], sb[j] >> (8 * in4)), prepare<EXACT>(va[i], sa[i] >> (8 * in4)), sum[i][j]);
+        }
     };
     for (uint32_t kb = 0; kb < nb; kb += 4) {
         block(kb, 0, s_codes0, s_codes1);
@@ -198,6 +242,7 @@ constexpr int kThinAhead = 4;
 template <class D, int TM>
 __global__ __launch_bounds__(kThinWaves * kWave) void k_product_thin(PackedMatrix a, PackedMatrix b, int64_t M, int64_t N, uint32_t nb,
                                                                    typename D::T* __restrict__ out, int64_t out_stride) {
+    constexpr bool kExact = Exact<D>::value;
     constexpr int kAhead = TM > 1 ? kThinAhead / 2 : kThinAhead;
     __shared__ floatx4 s_sum[kThinWaves][TM][kWave];
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, in16 = lane % 16, quarter = lane / 16;
@@ -235,7 +280,7 @@ __global__ __launch_bounds__(kThinWaves * kWave) void k_product_thin(PackedMatri
         for (int u = 0; u < kAhead; ++u) {
             if (k0 + u * kThinWaves < nb) {
 #pragma unroll
-                for (int i = 0; i < TM; ++i) sum[i] = multiply<Exact<D>::value, 0>(vb[u], sb[u], va[u][i], sa[u][i], sum[i]);
+                for (int i = 0; i < TM; ++i) sum[i] = multiply<kExact>(prepare<kExact>(vb[u], sb[u]), prepare<kExact>(va[u][i], sa[u][i]), sum[i]);
             }
         }
     }
