@@ -152,6 +152,13 @@ __device__ __forceinline__ uint32_t decode2(uint32_t c, float scale) {
     return __builtin_bit_cast(uint32_t, v);
 }
 
+// keeps the instructions that compute v in front of what follows
+__device__ __forceinline__ void pin(floatx4& v) {
+#ifdef __HIP_DEVICE_COMPILE__
+    asm volatile("" : "+v"(v));
+#endif
+}
+
 // Number `id` of `count` so that the ids that one XCD gets (id % 8, blocks are dealt out in turn) are consecutive numbers
 __device__ __forceinline__ uint32_t by_xcd(uint32_t id, uint32_t count) {
     const uint32_t xcd = id % 8, each = count / 8, more = count % 8;

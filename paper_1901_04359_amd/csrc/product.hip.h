@@ -75,13 +75,6 @@ __device__ __forceinline__ floatx4 multiply(const Operand<EXACT>& b, const Opera
         return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b.codes, a.codes, sum, 0, 0, 0, (int)b.scale, 0, (int)a.scale);
     }
 }
-// keeps the instructions that compute v in front of what follows
-__device__ __forceinline__ void pin(floatx4& v) {
-#ifdef __HIP_DEVICE_COMPILE__
-    asm volatile("" : "+v"(v));
-#endif
-}
-
 // A block computes BM x BN values with BM/WM x BN/WN waves of WM x WN each.  (Tiles of 128 x 128 with four waves, two blocks per
 // compute unit: 2048 x 4096 x 9216 to bf16 in 72 us = 2.1 PFLOP/s, 8192^3 in 509 us = 2.2; to fp32 146 and 929 us.  What
 // bounds them is LDS: per two blocks of 128 a compute unit reads 128 KB and writes 64 KB there, 1536 cycles at 128 bytes, where the matrix

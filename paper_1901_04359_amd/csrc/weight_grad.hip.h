@@ -84,8 +84,9 @@ constexpr int kGradRows = 32;               // rows of dY and X in one step
 // Tiles of 128 x 128 with four waves: where workers have few rows, writing dW bounds the call, and three blocks per compute unit
 // overlap one's stores with another's loads (16 workers, 64 rows each, 4096 x 9216: 2.4 GB, nearly all of it written, in 409 us =
 // 6.0 TB/s; a fill writes 6.9).  Tiles of 256 x 256 with eight waves for long sums in
-// bf16: half the LDS traffic and loads per product (16384 rows, 4096 x 4096: 463 us = 1.19 PFLOP/s, with tiles of 128 677 us);
-// there (kAhead) the next rows are staged while the matrix instructions run, also behind the last step, which would cost
+// bf16: half the LDS traffic and loads per product (16384 rows, 4096 x 4096: 464 us = 1.18 PFLOP/s, with tiles of 128 677 us);
+// there (kAhead) dY's columns are read, and the next rows staged, while the matrix instructions run (8192 rows, 8192 x 8192: 963 us,
+// all reads before them 1026; 64 rows a step need more than the registers), also behind the last step, which would cost
 // a quarter of the call where workers have two steps.
 // LINES: K is a multiple of 32, so dW's rows all begin at the same place in a memory line, but a layer may lie anywhere in its
 // worker's row.  Tiles that begin where lines do have whole lines to write, which go past the caches; a line written in two pieces
@@ -228,20 +229,35 @@ __global__ __launch_bounds__((BN / WN) * (BK / WK) * kWave, BN * BK > 128 * 128 
 #pragma unroll
             for (int i = 0; i < TK; ++i) x[i] = operand(s_x + buf * kGradRows * kPitchX, kPitchX, wk + i * 16);
             if constexpr (kAhead) {
-                stage(buf ^ 1, buf ^ 1);
-                load(buf ^ 1);
-            }
+                // dY's columns are read 16 at a time, while the products of the ones before run
+                static_assert(!kAhead || (kParts == 1 && TN > 4), "one part; columns to stage and to load beside");
+                const uint16_t* const in_d = s_d + buf * kGradRows * kPitchD;
+                bf16x8 d = operand(in_d, kPitchD, wn);
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int q = 0; q < kParts; ++q) {
-                bf16x8 d[TN];
+                for (int j = 0; j < TN; ++j) {
+                    const bf16x8 d_next_column = j + 1 < TN ? operand(in_d, kPitchD, wn + (j + 1) * 16) : d;
+                    if (j == 2) stage(buf ^ 1, buf ^ 1);
+                    if (j == 4) load(buf ^ 1);
 #pragma unroll
-                for (int j = 0; j < TN; ++j) d[j] = operand(s_d + (buf * kParts + q) * kGradRows * kPitchD, kPitchD, wn + j * 16);
+                    for (int i = 0; i < TK; ++i) sum[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[i], d, sum[i][j], 0, 0, 0);
+                    d = d_next_column;
+                    // these products here and not behind the next reads
 #pragma unroll
-                for (int i = 0; i < TK; ++i)
+                    for (int i = 0; i < TK; ++i) pin(sum[i][j]);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            } else {
 #pragma unroll
-                    for (int j = 0; j < TN; ++j) sum[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[i], d[j], sum[i][j], 0, 0, 0);
-            }
-            if constexpr (!kAhead) {
+                for (int q = 0; q < kParts; ++q) {
+                    bf16x8 d[TN];
+#pragma unroll
+                    for (int j = 0; j < TN; ++j) d[j] = operand(s_d + (buf * kParts + q) * kGradRows * kPitchD, kPitchD, wn + j * 16);
+#pragma unroll
+                    for (int i = 0; i < TK; ++i)
+#pragma unroll
+                        for (int j = 0; j < TN; ++j) sum[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[i], d[j], sum[i][j], 0, 0, 0);
+                }
                 if (step + 1 < steps) {
                     stage(buf ^ 1, buf ^ 1);
                     load(buf ^ 1);         // (rows behind the last one are not read)
