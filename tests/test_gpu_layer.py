@@ -364,6 +364,84 @@ def test_product_with_nan_in_16_bits(dtype):
         assert torch.equal(torch.nan_to_num(out.cpu()), torch.nan_to_num(want))
 
 
+# More than 512 tiles of 128 x 128 but at most 256 of 256 x 256: the product takes the large ones.  One block of 128 to ten, odd
+# numbers of them, a tile with a single row, and a single column.
+LARGE_PRODUCTS = [(2820, 2851, 1), (2830, 2817, 130), (257, 21890, 300), (2820, 2851, 385), (2945, 2690, 640), (21889, 257, 777), (2817, 2850, 1157)]
+
+
+def takes_large_tiles(M, N):
+    def tiles(side):
+        return -(-M // side) * -(-N // side)
+    return tiles(128) > 512 and tiles(256) <= 256
+
+
+@pytest.mark.parametrize("M,N,K", LARGE_PRODUCTS)
+def test_large_product_of_integers_is_exact(M, N, K):
+    import torch
+    from paper_1901_04359_amd import binding as B
+    assert takes_large_tiles(M, N)
+    a, b = int_packed(M, K, 1), int_packed(N, K, 2)
+    want = torch.from_numpy(ref.values(*a, K) @ ref.values(*b, K).T)
+    ga, gb = packed_on_gpu(*a, 1), packed_on_gpu(*b, 2)
+    ws = B.alloc_product_workspace(M, N, K)
+    for dtype in TYPES:
+        t = torch_type(dtype)
+        flat = torch.full((M * (N + 3) + 8,), math.nan, dtype=t, device="cuda")
+        out = flat[3:3 + M * (N + 3)].view(M, N + 3)[:, :N]
+        say(f"layer: large product {M}x{N}x{K} {dtype}")
+        B.gtopk_scaled_product(*ga, *gb, K, out, ws)
+        assert torch.equal(out.cpu(), want.float().to(t))
+        assert int(torch.isnan(flat).sum()) == 3 * M + 8            # what lies outside the rows is left alone
+
+
+def test_large_product_of_real_values():
+    """The bounds of the products above, for every 29th row (the bound of what eight products lose takes M N K values)."""
+    import torch
+    from paper_1901_04359_amd import binding as B
+    M, N, K = 2820, 2851, 1100
+    a, b = ref.pack(values_in(M, K, 7)), ref.pack(values_in(N, K, 8) / math.sqrt(K), tiles=True)
+    va, vb = ref.values(*a, K)[::29], ref.values(*b, K)
+    want, size = va @ vb.T, np.abs(va) @ np.abs(vb).T
+    cut = np.zeros(want.shape)
+    for k in range(0, K, 8):
+        cut += np.abs(va[:, None, k:k + 8] * vb[None, :, k:k + 8]).max(axis=2)
+    ga, gb = packed_on_gpu(*a), packed_on_gpu(*b)
+    for dtype in TYPES:
+        t = torch_type(dtype)
+        out = torch.zeros(M, N, dtype=t, device="cuda")
+        say(f"layer: large product of real values to {dtype}")
+        B.gtopk_scaled_product(*ga, *gb, K, out, B.alloc_product_workspace(M, N, K))
+        err = np.abs(out[::29].double().cpu().numpy() - want)
+        bound = (K + 4) * 2.0 ** -23 * size
+        if dtype == "f32":
+            assert (err <= bound).all()
+            assert np.linalg.norm(err) <= 2.0 ** -17 * np.linalg.norm(want)
+        else:
+            bound = (8 * 2.0 ** -13 * cut + bound) * (1 + half_step(t)) + half_step(t) * np.abs(want)
+            assert (err <= bound + (2.0 ** -25 if dtype == "f16" else 0.0)).all()
+            assert np.linalg.norm(err) <= 1.1 * half_step(t) * np.linalg.norm(want)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_large_product_with_nan_and_every_scale(dtype):
+    import torch
+    from paper_1901_04359_amd import binding as B
+    t = torch_type(dtype)
+    M, N, K = 2817, 2850, 640
+    a, b = int_packed(M, K, 3), int_packed(N, K, 4)
+    each = np.random.default_rng([M, N, K]).integers(7, 248, 5)
+    a[1][:] = each[None, :]
+    b[1][:] = np.clip(254 - each, 7, 247)[None, :]
+    a[0][M - 1, 7], b[0][N - 1, K - 1], b[1][N - 2, 2] = 0x7F, 0xFF, 255
+    want = torch.from_numpy(ref.values(*a, K) @ ref.values(*b, K).T).float().to(t)
+    out = torch.zeros(M, N, dtype=t, device="cuda")
+    say(f"layer: large product {dtype} with NaN and every scale")
+    B.gtopk_scaled_product(*packed_on_gpu(*a), *packed_on_gpu(*b), K, out, B.alloc_product_workspace(M, N, K))
+    got = out.cpu()
+    assert torch.equal(torch.isnan(got), torch.isnan(want))
+    assert torch.equal(torch.nan_to_num(got), torch.nan_to_num(want))
+
+
 # ---- weight gradient ------------------------------------------------------------------
 
 def begins(P, rows, kind, seed=0):
