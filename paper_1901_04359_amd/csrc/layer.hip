@@ -90,7 +90,7 @@ ProductPlan product_plan(int64_t M, int64_t N, int64_t K) {
     g.tiles_n = (uint32_t)ceil_div(N, 128);
     g.stride = ceil_div(N, 4) * 4;
     // A round of large tiles over the chip takes 1.67 times as long as one of small ones, two to a compute unit, and does twice as much (us,
-    // small / large: 8192^3 509 / 425; 4096^3 71 / 61; 8187 x 9216 x 4096 305 / 283, to fp32 538 / 491; 2048 x 4096 x 9216, half a round of large
+    // small / large: 8192^3 509 / 409; 4096^3 71 / 57; 8187 x 9216 x 4096 305 / 272, to fp32 538 / 494; 2048 x 4096 x 9216, half a round of large
     // ones, 72 / 111).
     const uint64_t tiles_large = (uint64_t)ceil_div(M, 256) * ceil_div(N, 256);
     g.large = !g.thin && 5 * ((tiles_large + 255) / 256) < 3 * (((uint64_t)g.tiles_m * g.tiles_n + 511) / 512);

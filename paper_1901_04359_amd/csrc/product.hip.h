@@ -29,12 +29,17 @@ struct PackedMatrix {
     uint32_t code_stride, scale_stride;     // bytes
 };
 
-// 16 bytes per lane from global memory into LDS, lane l to `to` + 16 l (`to` is uniform)
-__device__ __forceinline__ void load_to_lds16(const uint8_t* from, uint8_t* to) {
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+// Bytes from `from` + offset + at into LDS, 16 or 4 per lane, lane l's to `to` + 16 l or 4 l (all but `offset` are uniform).  Buffer loads add
+// the three by themselves; with a global load's address of 64 bits per lane the large tiles lose 4 % (8192^3 429 us, so 409).
+typedef __amdgpu_buffer_rsrc_t Source;
+__device__ __forceinline__ Source source(const uint8_t* from) {
+    return __builtin_amdgcn_make_buffer_rsrc((void*)from, 0, (int)0xFFFFFFFFu, 0x00027000);     // bytes, up to 2^32 of them
 }
-__device__ __forceinline__ void load_to_lds4(const uint8_t* from, uint8_t* to) {
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 4, 0, 0);
+__device__ __forceinline__ void load_to_lds16(Source from, uint32_t offset, uint32_t at, uint8_t* to) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)to, 16, (int)offset, (int)at, 0, 0);
+}
+__device__ __forceinline__ void load_to_lds4(Source from, uint32_t offset, uint32_t at, uint8_t* to) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)to, 4, (int)offset, (int)at, 0, 0);
 }
 
 // 8 codes as bf16 numbers, exactly
@@ -75,13 +80,17 @@ __device__ __forceinline__ floatx4 multiply(const Operand<EXACT>& b, const Opera
         return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b.codes, a.codes, sum, 0, 0, 0, (int)b.scale, 0, (int)a.scale);
     }
 }
-// A block computes BM x BN values with BM/WM x BN/WN waves of WM x WN each.  (Tiles of 128 x 128 with four waves, two blocks per
-// compute unit: 2048 x 4096 x 9216 to bf16 in 72 us = 2.1 PFLOP/s, 8192^3 in 509 us = 2.2; to fp32 146 and 929 us.  What
-// bounds them is LDS: per two blocks of 128 a compute unit reads 128 KB and writes 64 KB there, 1536 cycles at 128 bytes, where the matrix
-// instructions take 1024.  256 x 256 with four waves, which needs half of that, has one wave per SIMD and waits as much as it saves:
-// 142 and 493 us; 256 x 128 with eight 89 and 620; three LDS buffers of 256 x 128 with four 106 and 658.)  A block of 128 of the tile's rows of A and B
+
+// A block computes BM x BN values with BM/WM x BN/WN waves of WM x WN each.  A block of 128 of the tile's rows of A and B
 // goes straight from global memory into one of two LDS buffers while the matrix instructions work on the other; the scales
 // of four blocks go together (a word per row: fetched one by one they would be as many requests as the codes).
+// Tiles of 128 x 128 with four waves, two blocks per compute unit: 2048 x 4096 x 9216 to bf16 in 77 us = 2.0 PFLOP/s, 8192^3 in 509; to
+// fp32 147 and 929.  What bounds them is the way into LDS: of 8192^3's 509 us the loads alone take 407, the matrix instructions
+// alone 282, all but the loads 337.  Tiles of 256 x 256 with eight waves, one block per compute unit, need half the loads: 409 us = 2.7 PFLOP/s,
+// to fp32 773 = 1.4 (the matrix instructions of either type at 0.87 of what a library product of 8192^3 reaches).  Their waves read
+// A 16 rows at a time, for the registers (kStream).  Slower: 256 x 128 with eight waves 80 us for the first size, with three LDS buffers
+// 81; 256 x 256 with four waves 493 us for 8192^3; decoding B's rows for fp32 once per half block of A's 187 us for the first
+// size, nothing gained with large tiles.
 // In LDS a row's 16-byte pieces are exchanged by the row's number (piece p lies at p ^ (row / 2 % 8)): rows are 128
 // bytes apart, and without that a wave's lanes would read from an eighth of the banks.  Rows behind the
 // matrix's end are read as its last row and not written.  Grid: x the tiles, y shares of `share` blocks of 128 (a multiple of 4, or
@@ -102,7 +111,7 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * kWave, 1) void k_product(
     __shared__ __align__(128) uint8_t s_codes1[kStage];
     __shared__ __align__(128) uint8_t s_scales[2][kScaleLoads * kThreads * 4];      // a word per row: four blocks' scales
 
-    const uint32_t wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
     const uint32_t first = blockIdx.y * share, nb = blocks - first < share ? blocks - first : share;     // this share's blocks of 128
     out += blockIdx.y * M * out_stride;
     uint32_t tile_m, tile_n;
@@ -114,6 +123,7 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * kWave, 1) void k_product(
     const uint8_t* const b_base = b.codes + n0 * b.code_stride + (int64_t)first * kPackBlock;
     const uint32_t a_last = (uint32_t)(M - m0 < BM ? M - m0 - 1 : BM - 1), b_last = (uint32_t)(N - n0 < BN ? N - n0 - 1 : BN - 1);
 
+    const Source a_from = source(a_base), b_from = source(b_base);
     uint32_t offset[kLoads];
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
@@ -122,26 +132,24 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * kWave, 1) void k_product(
         const uint32_t row = of_a ? (r < a_last ? r : a_last) : (r - BM < b_last ? r - BM : b_last);
         offset[i] = row * (of_a ? a.code_stride : b.code_stride) + piece * 16;
     }
-    // (a row's scales can be read in fours to the end)
-    const uint8_t* scales_from[kScaleLoads];
+    // a word of four scales per row (which can be read in fours to the end); a wave's rows are of one matrix
+    Source scales_from[kScaleLoads];
+    uint32_t scale_offset[kScaleLoads];
 #pragma unroll
     for (int i = 0; i < kScaleLoads; ++i) {
         const uint32_t r = i * kThreads + threadIdx.x;
-        scales_from[i] = r < BM ? a.scales + (m0 + (r < a_last ? r : a_last)) * a.scale_stride
-                                : b.scales + (n0 + (r - BM < b_last ? r - BM : b_last)) * b.scale_stride;
-        scales_from[i] += first;           // (a multiple of 4)
+        const bool of_a = i * kThreads + wave * kWave < BM;
+        scales_from[i] = source((of_a ? a.scales + m0 * a.scale_stride : b.scales + n0 * b.scale_stride) + first);  // (a multiple of 4)
+        scale_offset[i] = of_a ? (r < a_last ? r : a_last) * a.scale_stride : (r - BM < b_last ? r - BM : b_last) * b.scale_stride;
     }
     auto fetch = [&](uint32_t kb, uint8_t* stage) __attribute__((always_inline)) {
-        uint32_t at = kb * kPackBlock;
-        asm("" : "+s"(at));                // scalar bases and offsets of 32 bits, not a pointer per load that is carried along
-        const uint8_t *a_from = a_base + at, *b_from = b_base + at;
 #pragma unroll
         for (int i = 0; i < kLoads; ++i)
-            load_to_lds16((i * kThreads / 8 < BM ? a_from : b_from) + offset[i], stage + (i * kThreads + wave * kWave) * 16);
+            load_to_lds16(i * kThreads / 8 < BM ? a_from : b_from, offset[i], kb * kPackBlock, stage + (i * kThreads + wave * kWave) * 16);
     };
     auto fetch_scales = [&](uint32_t kb, uint8_t* to) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < kScaleLoads; ++i) load_to_lds4(scales_from[i] + kb, to + (i * kThreads + wave * kWave) * 4);
+        for (int i = 0; i < kScaleLoads; ++i) load_to_lds4(scales_from[i], scale_offset[i], kb, to + (i * kThreads + wave * kWave) * 4);
     };
 
     const uint32_t wm = (wave / kWavesN) * WM, wn = (wave % kWavesN) * WN;
