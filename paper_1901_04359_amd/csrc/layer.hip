@@ -18,7 +18,7 @@ namespace {
 
 constexpr int64_t kMaxSide = 0x7FFFFFFF;            // rows and columns of a matrix
 constexpr int64_t kMaxCodeStride = 1 << 23;         // of a product's operands (also of their scales): a tile's rows at offsets of 32 bits
-constexpr int64_t kMaxTiles = (1 << 24) - 1;        // blocks of a product: fewer than 2^32 threads in a launch
+constexpr int64_t kMaxTiles = (1 << 24) - 1;        // of 128 x 128 in a product: fewer than 2^32 threads in a launch
 constexpr int64_t kMaxThinColumns = 1 << 26;
 constexpr uint64_t kMaxBlocks = 1u << 22;           // blocks of a launch; kernels walk what is left
 
@@ -234,7 +234,7 @@ int gtopk_activation_grad(const uint8_t* codes, int64_t code_stride, const uint8
 size_t gtopk_product_workspace_bytes(int64_t M, int64_t N, int64_t K) {
     if (!side_ok(M, 0) || !side_ok(N, 1) || !side_ok(K, 1) || K > kMaxCodeStride) return 0;
     const ProductPlan g = product_plan(M, N, K);
-    if (g.thin ? N > kMaxThinColumns : (int64_t)g.tiles_m * g.tiles_n > kMaxTiles) return 0;
+    if (g.thin ? N > kMaxThinColumns : ceil_div(M, 128) * ceil_div(N, 128) > kMaxTiles) return 0;
     return 256 + (g.shares > 1 ? (size_t)g.shares * M * g.stride * sizeof(float) : 0);
 }
 
