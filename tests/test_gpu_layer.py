@@ -442,6 +442,30 @@ def test_large_product_with_nan_and_every_scale(dtype):
     assert torch.equal(torch.nan_to_num(got), torch.nan_to_num(want))
 
 
+@pytest.mark.parametrize("M,N,far", [(257, 21890, "a"), (21890, 257, "b"), (300, 520, "a")])
+def test_product_of_rows_at_the_largest_stride(M, N, far):
+    """A tile's last row begins 255 * 2^23 bytes behind its first one, of large tiles and of small ones."""
+    import torch
+    from paper_1901_04359_amd import binding as B
+    K = 300
+    a, b = int_packed(M, K, 5), int_packed(N, K, 6)
+    want = torch.from_numpy(ref.values(*a, K) @ ref.values(*b, K).T).float()
+    ga, gb = packed_on_gpu(*a), packed_on_gpu(*b)
+    near = ga if far == "a" else gb
+    wide = []
+    for t in near:
+        w = torch.empty(t.shape[0] * 2 ** 23, dtype=torch.uint8, device="cuda").view(t.shape[0], 2 ** 23)[:, :t.shape[1]]
+        w.copy_(t)
+        wide.append(w)
+    ga, gb = (wide, gb) if far == "a" else (ga, wide)
+    ws = B.alloc_product_workspace(M, N, K)
+    for dtype in TYPES:
+        out = torch.zeros(M, N, dtype=torch_type(dtype), device="cuda")
+        say(f"layer: product {M}x{N}x{K} {dtype}, rows 2^23 bytes apart")
+        B.gtopk_scaled_product(*ga, *gb, K, out, ws)
+        assert torch.equal(out.cpu(), want.to(torch_type(dtype)))
+
+
 # ---- weight gradient ------------------------------------------------------------------
 
 def begins(P, rows, kind, seed=0):
