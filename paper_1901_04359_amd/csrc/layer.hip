@@ -120,7 +120,7 @@ struct GradPlan {
 constexpr uint64_t kMaxJobs = 0x3FFFFFFF;
 constexpr int64_t kGradShareRows = 256, kGradShareRowsBig = 512;    // rows of a share, at least
 // Tiles across in a band (tile_at) where products bound the call and L2 has to hold dY and X (in us, 4 / 8 / whole rows: 8192 rows, 4096 x
-// 4096 in fp32 803 / 812 / 872).  Whole rows of tiles where writing does, or where two tiles write one memory line.
+// 4096 in fp32, tiles of 128, 803 / 812 / 872).  Whole rows of tiles where writing does, or where two tiles write one memory line.
 constexpr uint32_t kGradBand = 4;
 constexpr int64_t kGradLinesK = 512, kGradLinesRows = 256;         // (rows times the parts of a dY value)
 GradPlan grad_plan_of(bool big, int64_t rows, int32_t P, int64_t N, int64_t K) {
@@ -313,11 +313,15 @@ int gtopk_weight_grad(const void* dy, int32_t dtype, int64_t dy_stride, const ui
     // Rows of whole memory lines (K a multiple of 32): tiles that begin where lines do, also in a row that does not, write past
     // the caches (LINES), the last of up to 31 more columns; where writing bounds the call, and from kGradLinesK on, where the
     // extra column of tiles is a small part.  (TB/s, 64 rows of every worker, without / with: 4096 x 9216 5.2 / 6.1; 1000 x 4096 4.4
-    // / 5.9; 2048 x 2048 4.3 / 6.3; the shares of 1501 rows by seven random cuts, 1000 x 4096 in fp32: 79 us without, 110 with.)
+    // / 5.9; 2048 x 2048 4.3 / 6.3; the shares of 1501 rows by seven random cuts, 1000 x 4096 in fp32: 79 us without, in tiles of 128, 110 with.)
     const bool aligned_rows = K % 32 == 0 && to_stride % 32 == 0 && aligned(to, 128);
     const bool writes = rows / P * (int64_t)value_parts(dtype) <= kGradLinesRows;
     const bool lines = !g.big && writes && (aligned_rows || (K % 32 == 0 && K >= kGradLinesK && !split));
-    const uint32_t tiles_k = lines && !aligned_rows ? (uint32_t)ceil_div(K + 31, 128) : g.tiles_k;
+    // An fp16 or fp32 dY is taken apart once per tile: twice as wide ones, with eight waves, where writing does not bound the call (us, 128 /
+    // 256 wide, fp32: 8192 rows, 4096 x 4096 805 / 666; 188 rows of 8 workers, 1000 x 4096 66 / 56; 150 rows of 4, 1000 x 1024 16.3 / 15.2; 200 of 16,
+    // 2000 x 128, where half of a tile is empty, 18.6 / 17.8.  bf16, 64 rows of 16 workers, 4096 x 9217: 484 / 505.)
+    const bool wide = !lines && dtype != GTOPK_BF16;
+    const uint32_t tiles_k = wide ? (uint32_t)ceil_div(K, 256) : lines && !aligned_rows ? (uint32_t)ceil_div(K + 31, 128) : g.tiles_k;
     const uint32_t jobs = g.tiles_n * tiles_k * (uint32_t)P * g.splits, band = writes || !aligned_rows ? tiles_k : kGradBand;
     hipStream_t st = (hipStream_t)stream;
     by_type(dtype, [&](auto d) {
@@ -327,10 +331,9 @@ int gtopk_weight_grad(const void* dy, int32_t dtype, int64_t dy_stride, const ui
                                scales, scale_stride, rows, row_begin, (uint32_t)P, N, K, to, to_stride, split ? 0 : accumulate != 0,
                                g.splits, split_stride, g.tiles_n, tiles_k, band, jobs);
         };
-        if constexpr (Parts<D>::n == 1) {
-            if (g.big) return launch(k_weight_grad<D, 256, 256, 128, 64, false>, 512);
-        }
         if (lines) launch(k_weight_grad<D, 128, 128, 64, 64, true>, 256);
+        else if constexpr (Parts<D>::n > 1) launch(k_weight_grad<D, 128, 256, 64, 64, false>, 512);
+        else if (g.big) launch(k_weight_grad<D, 256, 256, 128, 64, false>, 512);
         else launch(k_weight_grad<D, 128, 128, 64, 64, false>, 256);
     });
     if (split) {

@@ -83,7 +83,8 @@ constexpr int kGradRows = 32;               // rows of dY and X in one step
 // banks 16 lanes' pieces of 32 bytes fall on all of them.)
 // Tiles of 128 x 128 with four waves: where workers have few rows, writing dW bounds the call, and three blocks per compute unit
 // overlap one's stores with another's loads (16 workers, 64 rows each, 4096 x 9216: 2.4 GB, nearly all of it written, in 409 us =
-// 6.0 TB/s; a fill writes 6.9).  Tiles of 256 x 256 with eight waves for long sums in
+// 6.0 TB/s; a fill writes 6.9).  Tiles of 128 x 256 with eight waves where they don't and dY is fp16 or fp32, as taking it apart is what costs there
+// (half of the steps' vector instructions).  Tiles of 256 x 256 with eight waves for long sums in
 // bf16: half the LDS traffic and loads per product (16384 rows, 4096 x 4096: 464 us = 1.18 PFLOP/s, with tiles of 128 677 us);
 // there (kAhead) dY's columns are read, and the next rows staged, while the matrix instructions run (8192 rows, 8192 x 8192: 963 us,
 // all reads before them 1026; 64 rows a step need more than the registers), also behind the last step, which would cost
@@ -92,7 +93,7 @@ constexpr int kGradRows = 32;               // rows of dY and X in one step
 // worker's row.  Tiles that begin where lines do have whole lines to write, which go past the caches; a line written in two pieces
 // by two blocks costs more than twice (4096 x 9216 from an odd place: 484 us without LINES).
 template <class D, int BN, int BK, int WN, int WK, bool LINES>
-__global__ __launch_bounds__((BN / WN) * (BK / WK) * kWave, BN * BK > 128 * 128 ? 1 : Parts<D>::n == 1 ? 3 : 2) void k_weight_grad(
+__global__ __launch_bounds__((BN / WN) * (BK / WK) * kWave, BN * BK == 256 * 256 ? 1 : Parts<D>::n == 1 ? 3 : 2) void k_weight_grad(
         const typename D::T* __restrict__ dy, int64_t dy_stride, const uint8_t* __restrict__ codes, int64_t code_stride,
         const uint8_t* __restrict__ scales, int64_t scale_stride, int64_t rows, const int32_t* __restrict__ begin, uint32_t P,
         int64_t N, int64_t K, float* __restrict__ grad, int64_t grad_stride, int accumulate, uint32_t splits, int64_t split_stride,
@@ -104,7 +105,7 @@ __global__ __launch_bounds__((BN / WN) * (BK / WK) * kWave, BN * BK > 128 * 128 
     constexpr int kLoadsD = kGradRows * BN / 8 / kThreads, kLoadsX = kGradRows * BK / 16 / kThreads;
     static_assert(kLoadsD * kThreads * 8 == kGradRows * BN && kLoadsX * kThreads * 16 == kGradRows * BK, "whole loads");
     static_assert(BK % kPackBlock == 0, "a lane's 16 codes lie in one block of 128, or in two with LINES");
-    constexpr bool kAhead = BN * BK > 128 * 128;
+    constexpr bool kAhead = BN * BK == 256 * 256;
     constexpr int kPitchOut = WK + 4;                                      // floats
     static_assert((BN / WN) * kWavesK * 16 * kPitchOut * 2 <= 2 * kGradRows * (kParts * kPitchD + kPitchX), "the result's rows fit the same memory");
     __shared__ __align__(16) uint16_t s_rows[2 * kGradRows * (kParts * kPitchD + kPitchX)];
@@ -116,7 +117,7 @@ __global__ __launch_bounds__((BN / WN) * (BK / WK) * kWave, BN * BK > 128 * 128 
     for (uint32_t id = blockIdx.x; id < jobs; id += gridDim.x) {
         // Equal shares: an XCD gets whole workers, whose rows then lie in its L2 (TB/s with 64 rows of every worker, whole / spread out:
         // 4096 x 1024 5.9 / 5.5, 1000 x 4096 5.8 / 5.3, 4096 x 9217 4.9 / 4.6, larger ones alike).  Uneven ones: every worker's tiles are
-        // spread over all XCDs (the shares of 1501 rows by seven random cuts, 1000 x 4096 in fp32: 76 us, by XCD 167).
+        // spread over all XCDs (the shares of 1501 rows by seven random cuts, 1000 x 4096 in fp32, tiles of 128: 76 us, by XCD 167).
         const uint32_t tiles = tiles_n * tiles_k, spread = begin ? tiles * splits : jobs, at = id / spread * spread;
         uint32_t job = at + by_xcd(id - at, spread);
         uint32_t tile_n, tile_k;
