@@ -264,6 +264,9 @@ int gtopk_dense_topk(const float* dense, int64_t m, int32_t k, uint32_t* g_idx, 
  *                               >= ceil(cols / 128); the bytes behind the last block's are not written, and what they hold
  *                               does not matter (they may be read, up to the next multiple of 4).
  *   The value of a code c in a block of scale s is e4m3(c) * 2^(s - 127).  codes is 16-byte aligned, scales 4-byte.
+ *   A magnitude of 2^128 or more (scales from 247 on; the pack calls make one, 2^128, of a finite value from 1.9375 * 2^127 on)
+ *   is more than fp32 holds: gtopk_unpack and gtopk_activation_grad take it as an infinity, with f and f' what they tend to
+ *   there.
  * Dense matrices (x, dy, out, dx, grad) have contiguous rows at any stride >= their columns and need the
  * alignment of one value only, as a layer may lie anywhere in a flat row.  dtype is one of gtopk_dtype.
  * Sizes: rows and columns 1 .. 2^31 - 1; rows (M of the product) may also be 0: then there is nothing to

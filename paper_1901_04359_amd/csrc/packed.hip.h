@@ -272,17 +272,23 @@ __device__ __forceinline__ float normal_tail(float x, float& bell) {
     return p * t;
 }
 
+// Values of 2^128 and more decode to infinities.  Where a factor falls to 0 far out (from |x| = 104 on at the latest), x beside it is cut off
+// behind that, as an infinity times 0 is NaN.  (A NaN of x is in the other factor.)
+constexpr float kFarOut = 1e4f;
+__device__ __forceinline__ float near_size(float x) { return fminf(fabsf(x), kFarOut); }
+__device__ __forceinline__ float near_value(float x) { return fminf(fmaxf(x, -kFarOut), kFarOut); }
+
 // (a NaN gives NaN in every branch)
 template <int ACT>
 __device__ __forceinline__ float act_value(float x) {
     if constexpr (ACT == GTOPK_ACT_RELU) return x < 0.0f ? 0.0f : x;
     if constexpr (ACT == GTOPK_ACT_TANH) return tanh_of(x);
     if constexpr (ACT == GTOPK_ACT_SIGMOID) return logistic(x);
-    if constexpr (ACT == GTOPK_ACT_SILU) return x * logistic(x);
+    if constexpr (ACT == GTOPK_ACT_SILU) return fmaxf(x, -kFarOut) * logistic(x);
     if constexpr (ACT == GTOPK_ACT_GELU) {
         float bell;                                // x Phi(x) = max(x, 0) - |x| Phi(-|x|)
         const float tail = normal_tail(x, bell);
-        return fmaf(-fabsf(x) * bell, tail, fmaxf(x, 0.0f));
+        return fmaf(-near_size(x) * bell, tail, fmaxf(x, 0.0f));
     }
     return x;
 }
@@ -295,12 +301,12 @@ __device__ __forceinline__ float act_slope(float x) {
     }
     if constexpr (ACT == GTOPK_ACT_SIGMOID || ACT == GTOPK_ACT_SILU) {
         const float e = exp_of(-fabsf(x)), r = reciprocal(1.0f + e), slope = e * r * r;
-        return ACT == GTOPK_ACT_SIGMOID ? slope : fmaf(x, slope, x < 0.0f ? e * r : r);
+        return ACT == GTOPK_ACT_SIGMOID ? slope : fmaf(near_value(x), slope, x < 0.0f ? e * r : r);
     }
     if constexpr (ACT == GTOPK_ACT_GELU) {
         float bell;
         const float below = normal_tail(x, bell) * bell;
-        return fmaf(x * 0.39894228040143268f, bell, x < 0.0f ? below : 1.0f - below);
+        return fmaf(near_value(x) * 0.39894228040143268f, bell, x < 0.0f ? below : 1.0f - below);
     }
     return x == x ? 1.0f : x;
 }
