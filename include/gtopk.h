@@ -266,7 +266,7 @@ int gtopk_dense_topk(const float* dense, int64_t m, int32_t k, uint32_t* g_idx, 
  *   The value of a code c in a block of scale s is e4m3(c) * 2^(s - 127).  codes is 16-byte aligned, scales 4-byte.
  *   A magnitude of 2^128 or more (scales from 247 on; the pack calls make one, 2^128, of a finite value from 1.9375 * 2^127 on)
  *   is more than fp32 holds: gtopk_unpack and gtopk_activation_grad take it as an infinity, with f and f' what they tend to
- *   there.
+ *   there; so do products to fp32 and weight gradients (a 16-bit result of a product takes it as it is).
  * Dense matrices (x, dy, out, dx, grad) have contiguous rows at any stride >= their columns and need the
  * alignment of one value only, as a layer may lie anywhere in a flat row.  dtype is one of gtopk_dtype.
  * Sizes: rows and columns 1 .. 2^31 - 1; rows (M of the product) may also be 0: then there is nothing to
@@ -320,7 +320,8 @@ int gtopk_activation_grad(const uint8_t* codes, int64_t code_stride, const uint8
  * out = A B^T for packed A (M x K) and packed B (N x K): out[m][n] = sum over k of A[m][k] * B[n][k], rounded once to
  * dtype.  Forward pass of a layer: A its packed input, B its packed weights; input gradient: A the packed output
  * gradient, B the transposed packed weights.
- *   GTOPK_F32:  products are exact, sums are fp32 (magnitudes below 2^-126 may be rounded to a multiple of 2^-133).
+ *   GTOPK_F32:  products of values below 2^128 are exact, sums are fp32 (values below 2^-126 may be rounded to a multiple of
+ *               2^-133).
  *   GTOPK_BF16, GTOPK_F16: twice as fast.  The eight products of k = 8 j .. 8 j + 7 are exact, but each is cut
  *               off at 2^-13 of the largest of the eight (its leading bit); all further sums are fp32.
  *   Strides of codes and scales (and so K) of at most 2^23; fewer than 2^24 tiles of 128 x 128 in out, for M <= 32
@@ -346,7 +347,9 @@ int gtopk_scaled_product(const uint8_t* a_codes, int64_t a_code_stride, const ui
  *   P : 1 .. 32768;  grad_stride : >= N*K if P > 1 (the row length m of the step)
  *   ws : gtopk_weight_grad_workspace_bytes(rows, P, N, K) bytes (0 if the sizes are invalid)
  * Sums are fp32, in an order that depends on the arguments only; dY enters exactly, whatever its type (an fp16 or fp32
- * value as a sum of two or three bf16 numbers), but for parts below 2^-126, which may be taken as 0.
+ * value as a sum of two or three bf16 numbers), but for parts below 2^-126, which may be taken as 0.  X enters exactly from 2^-126
+ * up to 2^128: values below may be rounded to a multiple of 2^-133, and one of 2^128 or more, or a NaN, makes the sums that it enters
+ * infinite or NaN.
  */
 size_t gtopk_weight_grad_workspace_bytes(int64_t rows, int32_t P, int64_t N, int64_t K);
 int gtopk_weight_grad(const void* dy, int32_t dtype, int64_t dy_stride, const uint8_t* codes, int64_t code_stride,
