@@ -238,17 +238,35 @@ __global__ __launch_bounds__(kPackThreads) void k_pack_rows(
 
 // ---- f and f' of the layer's activation, in 32 bits -----------------------------------
 // Written for the rate of the memory: some twenty operations per value, each function from one exponential and one reciprocal.
+// FINE, for fp32 results: the exponentials' arguments are corrected for what their own rounding lost, as results would otherwise be off by |x| (GELU:
+// x^2) 2^-24 far out; 16-bit ones are rounded to 2^-9 or 2^-12, more than that wherever the result is not 0.  (8192 x 4096 to fp32 with / without
+// the correction, in us: unpack tanh 29.2 / 27.7, GELU 31.1 / 27.8, logistic and SiLU 28; activation gradients all 50, bound by HBM.)
 
-__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896341f); }   // off by 2^-23 max(1, |x|)
+// 2^(t + rest)
+template <bool FINE>
+__device__ __forceinline__ float exp2_of(float t, float rest) {
+    const float e = __builtin_amdgcn_exp2f(t);                 // off by 2^-23, 0 for a result below 2^-126
+    return FINE ? fmaf(e, rest * 0.69314718055994531f, e) : e;
+}
+// e^-a of an a >= 0
+template <bool FINE>
+__device__ __forceinline__ float exp_minus(float a) {
+    constexpr float kLog2E = 1.44269504088896341f, kLog2EBehind = (float)(1.44269504088896341 - (double)kLog2E);
+    if constexpr (FINE) a = a > 128.0f ? 128.0f : a;           // (an infinity has no remainder; a NaN stays)
+    const float t = a * -kLog2E;
+    return exp2_of<FINE>(t, FINE ? fmaf(a, -kLog2EBehind, fmaf(a, -kLog2E, -t)) : 0.0f);
+}
 __device__ __forceinline__ float reciprocal(float x) { return __builtin_amdgcn_rcpf(x); }                     // off by 2^-23
 // 1 / (1 + e^-x), without cancellation at either end
+template <bool FINE>
 __device__ __forceinline__ float logistic(float x) {
-    const float e = exp_of(-fabsf(x)), r = reciprocal(1.0f + e);
+    const float e = exp_minus<FINE>(fabsf(x)), r = reciprocal(1.0f + e);
     return x < 0.0f ? e * r : r;
 }
 // tanh x = (1 - e) / (1 + e) with e = exp(-2 |x|); below 1/4, where 1 - e cancels, the Taylor series to x^9 (the next term is 2^-26 there)
+template <bool FINE>
 __device__ __forceinline__ float tanh_of(float x) {
-    const float e = exp_of(-2.0f * fabsf(x)), far = copysignf((1.0f - e) * reciprocal(1.0f + e), x), s = x * x;
+    const float e = exp_minus<FINE>(2.0f * fabsf(x)), far = copysignf((1.0f - e) * reciprocal(1.0f + e), x), s = x * x;
     float p = fmaf(s, 62.0f / 2835.0f, -17.0f / 315.0f);
     p = fmaf(s, p, 2.0f / 15.0f);
     p = fmaf(s, p, -1.0f / 3.0f);
@@ -256,10 +274,15 @@ __device__ __forceinline__ float tanh_of(float x) {
 }
 // Phi(-|x|) = erfc(z) / 2 with z = |x| / sqrt 2, and e^(-x^2 / 2), as tail * bell.  For z >= 0, erfc(z) = e^(-z^2) t p(t) with
 // t = 1 / (1 + 0.3 z); p has degree 8, fitted to erfc(z) e^(z^2) / t for z up to 10.5 with weights that level the relative error:
-// 2^-25, evaluated in fp32 7e-7 up to z = 3.  (p is halved here.)
+// 2^-24.3 in 64 bits, evaluated in fp32 at most 9e-7, that with the reciprocal a step off.  (p is halved here.)
+template <bool FINE>
 __device__ __forceinline__ float normal_tail(float x, float& bell) {
+    constexpr double kPower = -0.72134752044448170;            // e^(-x^2 / 2) = 2^(kPower x^2)
+    constexpr float kNear = (float)kPower, kBehind = (float)(kPower - (double)kNear);
     const float t = reciprocal(fmaf(0.3f * 0.70710678118654752f, fabsf(x), 1.0f));
-    bell = __builtin_amdgcn_exp2f(x * x * -0.72134752044448170f);
+    const float a = FINE && fabsf(x) > 16.0f ? 16.0f : x;      // (2^-184 there; a NaN stays)
+    const float square = a * a, power = square * kNear;
+    bell = exp2_of<FINE>(power, FINE ? fmaf(square, kBehind, fmaf(fmaf(a, a, -square), kNear, fmaf(square, kNear, -power))) : 0.0f);
     float p = -0.06477917730808258f;
     p = fmaf(p, t, 0.2428741753101349f);
     p = fmaf(p, t, -0.256346195936203f);
@@ -279,37 +302,39 @@ __device__ __forceinline__ float near_size(float x) { return fminf(fabsf(x), kFa
 __device__ __forceinline__ float near_value(float x) { return fminf(fmaxf(x, -kFarOut), kFarOut); }
 
 // (a NaN gives NaN in every branch)
-template <int ACT>
+template <int ACT, bool FINE>
 __device__ __forceinline__ float act_value(float x) {
     if constexpr (ACT == GTOPK_ACT_RELU) return x < 0.0f ? 0.0f : x;
-    if constexpr (ACT == GTOPK_ACT_TANH) return tanh_of(x);
-    if constexpr (ACT == GTOPK_ACT_SIGMOID) return logistic(x);
-    if constexpr (ACT == GTOPK_ACT_SILU) return fmaxf(x, -kFarOut) * logistic(x);
+    if constexpr (ACT == GTOPK_ACT_TANH) return tanh_of<FINE>(x);
+    if constexpr (ACT == GTOPK_ACT_SIGMOID) return logistic<FINE>(x);
+    if constexpr (ACT == GTOPK_ACT_SILU) return fmaxf(x, -kFarOut) * logistic<FINE>(x);
     if constexpr (ACT == GTOPK_ACT_GELU) {
         float bell;                                // x Phi(x) = max(x, 0) - |x| Phi(-|x|)
-        const float tail = normal_tail(x, bell);
+        const float tail = normal_tail<FINE>(x, bell);
         return fmaf(-near_size(x) * bell, tail, fmaxf(x, 0.0f));
     }
     return x;
 }
-template <int ACT>
+template <int ACT, bool FINE>
 __device__ __forceinline__ float act_slope(float x) {
     if constexpr (ACT == GTOPK_ACT_RELU) return x > 0.0f ? 1.0f : x <= 0.0f ? 0.0f : x;
     if constexpr (ACT == GTOPK_ACT_TANH) {         // 1 - tanh^2 = 4 e / (1 + e)^2
-        const float e = exp_of(-2.0f * fabsf(x)), r = reciprocal(1.0f + e);
+        const float e = exp_minus<FINE>(2.0f * fabsf(x)), r = reciprocal(1.0f + e);
         return 4.0f * e * r * r;
     }
     if constexpr (ACT == GTOPK_ACT_SIGMOID || ACT == GTOPK_ACT_SILU) {
-        const float e = exp_of(-fabsf(x)), r = reciprocal(1.0f + e), slope = e * r * r;
+        const float e = exp_minus<FINE>(fabsf(x)), r = reciprocal(1.0f + e), slope = e * r * r;
         return ACT == GTOPK_ACT_SIGMOID ? slope : fmaf(near_value(x), slope, x < 0.0f ? e * r : r);
     }
     if constexpr (ACT == GTOPK_ACT_GELU) {
         float bell;
-        const float below = normal_tail(x, bell) * bell;
+        const float below = normal_tail<FINE>(x, bell) * bell;
         return fmaf(near_value(x) * 0.39894228040143268f, bell, x < 0.0f ? below : 1.0f - below);
     }
     return x == x ? 1.0f : x;
 }
+
+template <class D> constexpr bool kFine = sizeof(typename D::T) == 4;
 
 template <class D, int ACT>
 __global__ __launch_bounds__(kPackThreads) void k_unpack(
@@ -325,7 +350,7 @@ __global__ __launch_bounds__(kPackThreads) void k_unpack(
         float v[kLaneVals];
         decode8(c[u], scale_value(s[u]), v);
 #pragma unroll
-        for (int j = 0; j < kLaneVals; ++j) v[j] = act_value<ACT>(v[j]);
+        for (int j = 0; j < kLaneVals; ++j) v[j] = act_value<ACT, kFine<D>>(v[j]);
         store_row<D>(out + row * stride + col, g.cols - col, v);
     });
 }
@@ -347,7 +372,7 @@ __global__ __launch_bounds__(kPackThreads) void k_activation_grad(
         float v[kLaneVals];
         decode8(c[u], scale_value(s[u]), v);
 #pragma unroll
-        for (int j = 0; j < kLaneVals; ++j) v[j] = (float)in[u][j] * act_slope<ACT>(v[j]);
+        for (int j = 0; j < kLaneVals; ++j) v[j] = (float)in[u][j] * act_slope<ACT, kFine<D>>(v[j]);
         store_row<D>(dx + row * dx_stride + col, g.cols - col, v);
     });
 }

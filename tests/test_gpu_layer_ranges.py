@@ -47,6 +47,60 @@ def test_activation_of_values_that_fp32_cannot_hold(act, dtype):
         assert bool(((got - want).abs()[fine] <= (32 * 2.0 ** -24 + 2 * half_step(t)) * want.abs()[fine]).all()), act
 
 
+# ---- the tails of the activation functions --------------------------------------------
+
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("dtype", TYPES)
+def test_activation_relative_to_its_value(act, dtype):
+    """Every code at scales that lead from 2^-69 far behind the last argument at which an exponential is not 0: errors relative to f and f'.
+
+    In fp32 an exponential of a corrected argument is off by 4 u (1 step of 2 u of the instruction, the correction's rounding and
+    the last fma), a reciprocal by 2 u, a sum or product by 1 u.  With e = exp(-|x|) (tanh: exp(-2 |x|)), whose error
+    enters with the factor in brackets:
+      logistic  1 / (1 + e): 4 (1/2) + 1 + 2 = 5;  e / (1 + e): 4 (1) + 1 + 2 + 1 = 8;  SiLU 1 more
+      tanh      (1 - e) / (1 + e), |x| >= 1/4: 4 (2 e / (1 - e^2) <= 1.93) + 1 + 1 + 2 + 1 = 13; below a series to x^9, which leaves out
+                1382/155925 x^10 < 0.2 u, and some roundings
+      slopes    4 e / (1 + e)^2 and e / (1 + e)^2: 4 (1) + 2 (1 + 2) + 3 = 13; SiLU's is the sum of two such terms, and is held against
+                the sum of their magnitudes, as is GELU's
+      GELU      |x| bell tail: 4 for the bell, 3 roundings, and the tail's polynomial with its reciprocal 14.4 (all arguments in steps of 3e-5,
+                emulated with the reciprocal a step off to either side): 22
+    Below: 16 u, GELU 24 u.  For 16 bits the exponentials' arguments are not corrected: up to |x| u more, in GELU x^2 u.  An
+    exponential below 2^-126 may be 0."""
+    import torch
+    from paper_1901_04359_amd import binding as B
+    t = torch_type(dtype)
+    codes = np.tile(np.concatenate([np.arange(0x7F), [0], np.arange(0x80, 0xFF), [0]]).astype(np.uint8), (75, 1))
+    scales = np.repeat(np.arange(67, 142, dtype=np.uint8)[:, None], 2, axis=1)
+    scales[0] = 60
+    x = ref.values(codes, scales, 256)
+    x[x == 0] = 0.0
+    c, s = packed_on_gpu(codes, scales)
+    out, dx = torch.zeros(75, 256, dtype=t, device="cuda"), torch.zeros(75, 256, dtype=t, device="cuda")
+    say(f"layer: {act} {dtype} relative to its value")
+    B.gtopk_unpack(c, s, act, out)
+    B.gtopk_activation_grad(c, s, act, torch.ones(75, 256, dtype=t, device="cuda"), dx)
+    f, slope = ref.act(act, x), ref.slope(act, x)
+    size = np.abs(slope)
+    logistic = ref.act("sigmoid", x)
+    if act == "silu":
+        size = logistic + np.abs(x) * logistic * ref.act("sigmoid", -x)
+    if act == "gelu":
+        size = np.abs(ref.act("gelu", x) / np.where(x == 0, 1.0, x)) + np.abs(x) * np.exp(-x * x / 2) / math.sqrt(2 * math.pi)
+        size[x == 0] = 0.5
+    u, floor = 2.0 ** -24, 2.0 ** -126 * np.maximum(1.0, np.abs(x))
+    rel = (0.0 if act in ("none", "relu") else 24 * u if act == "gelu" else 16 * u) + np.zeros_like(x)
+    if dtype != "f32":
+        rel = rel + u * (np.minimum(np.abs(x), 128) + np.minimum(x * x, 256)) + half_step(t)
+        floor = floor + (2.0 ** -25 if dtype == "f16" else 0.0)
+    for got, want, of in ((out, f, np.abs(f)), (dx, slope, size)):
+        g = got.double().cpu().numpy()
+        fits = np.abs(want) < torch.finfo(t).max              # (fp16 ends at 65504)
+        assert np.isinf(g[~fits]).all()
+        off = np.abs(g - want) - floor
+        bad = fits & (off > rel * of)
+        assert not bad.any(), (act, x[bad][:5], g[bad][:5], want[bad][:5])
+
+
 # ---- products and weight gradients of every scale -------------------------------------
 
 def int_codes(rows, cols, seed, unit=1.0):
