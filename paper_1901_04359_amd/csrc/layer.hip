@@ -118,7 +118,8 @@ struct GradPlan {
     uint64_t jobs;
 };
 constexpr uint64_t kMaxJobs = 0x3FFFFFFF;
-constexpr int64_t kGradShareRows = 256, kGradShareRowsBig = 512;    // rows of a share, at least
+constexpr int64_t kGradShareRows = 256, kGradShareRowsBig = 1024;   // rows of a share, at least
+constexpr int64_t kGradRowsBig = 512;                               // rows of a worker from which on large tiles are weighed
 // Tiles across in a band (tile_at) where products bound the call and L2 has to hold dY and X (in us, 4 / 8 / whole rows: 8192 rows, 4096 x
 // 4096 in fp32, tiles of 128, 803 / 812 / 872).  Whole rows of tiles where writing does, or where two tiles write one memory line.
 constexpr uint32_t kGradBand = 4;
@@ -137,16 +138,21 @@ GradPlan grad_plan_of(bool big, int64_t rows, int32_t P, int64_t N, int64_t K) {
     g.jobs = blocks * g.splits;
     return g;
 }
-// Large tiles for sums of at least kGradShareRowsBig rows in bf16 (an fp16 or fp32 dY's two or three parts do not fit the
-// registers beside their sums), if they keep three quarters of the chip at work and add at most a quarter to
-// what the small ones compute behind the edges.  (In us, small / large: 16384 rows, 1024 x 1024 59 / 55; 4096 x 4096 677 / 463;
-// 64 rows of 16 workers, 4096 x 9216: 392 / 533.)
+// Large tiles in bf16 (an fp16 or fp32 dY's two or three parts do not fit the registers beside their sums).
+// Without shares: a round of large tiles over the chip takes as long as 3.5 small ones per compute unit (us with 2048 rows: 70 a round; small ones
+// 96, 108, 124, 147, 165, 181, 239 with 4, 5, 6, 7, 8, 9, 12 per compute unit), with fewer rows somewhat longer.  (small / large, 512 and 2048 rows: 4096
+// x 4096 35 / 30 and 97 / 70; 5120 x 5120 52 / 52 and 147 / 132; 4096 x 5120 39 / 51 and 108 / 136; 4096 x 9216 67 / 82 and 182 / 207; 8192 x 8192
+// 108 / 112 and 316 / 289; 256 rows of 16 workers, 4096 x 4096 307 / 338.)
+// In shares: from 1024 rows per share on, if they keep three quarters of the chip at work; from 2048 on if small ones need no shares.  (One worker, rows per large
+// share: 1024 x 1024 512: 39 / 42, 1024: 59 / 55; 2048 x 2048 512: 41 / 43, 1024: 62 / 57; 2048 x 4096 1024: 52 / 60, 2048: 95 / 87; 4 workers, 1024 x 1024
+// 512: 40 / 43, 1024: 61 / 57.)
 GradPlan grad_plan(bool bf16, int64_t rows, int32_t P, int64_t N, int64_t K) {
     const GradPlan small = grad_plan_of(false, rows, P, N, K);
-    if (!bf16 || rows / P < kGradShareRowsBig) return small;
+    if (!bf16 || rows / P < kGradRowsBig) return small;
     const GradPlan large = grad_plan_of(true, rows, P, N, K);
-    const bool fits = 4 * 4 * (uint64_t)large.tiles_n * large.tiles_k <= 5 * (uint64_t)small.tiles_n * small.tiles_k;
-    return fits && large.jobs >= 192 ? large : small;
+    const bool gain = large.splits == 1 ? 7 * ((large.jobs + 255) / 256) <= 2 * ((small.jobs + 255) / 256)
+                                        : large.jobs >= 192 && (small.splits > 1 || rows / P / large.splits >= 2 * kGradShareRowsBig);
+    return gain ? large : small;
 }
 
 }  // namespace

@@ -1,0 +1,100 @@
+"""Weight gradients at the sizes that decide which tiles they take: large tiles, without shares of the rows and with.  The rules are written out here as well (`plan`), so that a
+change to them does not silently leave a kernel without its test.
+
+Inputs are small integers, sums are exact in fp32 in every order, and the results are compared to the bit."""
+import numpy as np
+import pytest
+
+from tests import layer_reference as ref
+from tests.gpu_harness import say
+from tests.test_gpu_layer import TYPES, torch_type
+
+pytestmark = pytest.mark.gpu
+
+PARTS = {"bf16": 1, "f16": 2, "f32": 3}
+
+
+def cdiv(a, b):
+    return -(-a // b)
+
+
+def tiles_of(side, P, rows, N, K):
+    """(tiles, shares of the rows) with tiles of this side"""
+    tiles = cdiv(N, side) * cdiv(K, side) * P
+    shares = max(1, min(rows // P // (1024 if side == 256 else 256), (256 if side == 256 else 512) // tiles))
+    return tiles, shares
+
+
+def plan(dtype, P, rows, N, K, aligned):
+    """(kernel, shares of the rows) that a weight gradient takes, but for results along memory lines"""
+    each = rows // P
+    small, shares = tiles_of(128, P, rows, N, K)
+    if dtype == "bf16" and each >= 512:
+        large, large_shares = tiles_of(256, P, rows, N, K)
+        if large_shares == 1:
+            gain = 7 * cdiv(large, 256) <= 2 * cdiv(small * shares, 256)
+        else:
+            gain = large * large_shares >= 192 and (shares > 1 or each // large_shares >= 2048)
+        if gain:
+            return "large", large_shares
+    return ("small" if dtype == "bf16" else "wide"), shares
+
+
+def integer_case(P, rows, N, K, dtype, seed=0):
+    """dY [rows][N] and X [rows][K] of small integers on the GPU, X also packed"""
+    import torch
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(1000 * P + 10 * rows + seed)
+    dy = torch.randint(-3, 4, (rows, N), device="cuda", generator=gen, dtype=torch.int32).to(torch_type(dtype))
+    x = torch.randint(-2, 3, (rows, K), device="cuda", generator=gen, dtype=torch.int64)
+    nb = cdiv(K, 128)
+    codes = torch.zeros(rows, nb * 128, dtype=torch.uint8, device="cuda")
+    codes[:, :K] = torch.from_numpy(ref.encode(np.arange(-2.0, 3.0))).cuda()[x + 2]
+    scales = torch.randint(126, 129, (rows, cdiv(nb, 4) * 4), device="cuda", generator=gen, dtype=torch.int32).to(torch.uint8)
+    f = torch.exp2(scales[:, :nb].double() - 127.0).repeat_interleave(128, dim=1)[:, :K]
+    return dy, codes, scales, x.double() * f
+
+
+def check(P, rows, N, K, dtype, behind, gap, begin=None, again=True):
+    """Into rows of 7s, `behind` values behind their start and `gap` before the next; then onto what is there."""
+    import torch
+    from paper_1901_04359_amd import binding as B
+    dy, codes, scales, x = integer_case(P, rows, N, K, dtype)
+    at = begin or [rows // P * w for w in range(P + 1)]
+    base = torch.full((32 + P * (behind + N * K + gap) + 32,), 7.0, device="cuda")
+    assert base.data_ptr() % 128 == 0
+    inside = base[32:-32].view(P, behind + N * K + gap)
+    grad = inside[:, behind:behind + N * K].unflatten(1, (N, K))
+    ws = B.alloc_weight_grad_workspace(rows, P, N, K)
+    ws.fill_(0xFF)
+    row_begin = None if begin is None else torch.tensor(begin, dtype=torch.int32, device="cuda")
+    say(f"layer: weight_grad {dtype} P {P} rows {rows} {N}x{K} behind {behind} gap {gap}")
+    for times in (1, 2) if again else (1,):
+        B.gtopk_weight_grad(dy, codes, scales, row_begin, grad, times == 2, ws)
+        for w in range(P):
+            want = (dy[at[w]:at[w + 1]].double().t().contiguous() @ x[at[w]:at[w + 1]]).mul_(times)
+            assert float(want.abs().max()) < 2 ** 23
+            assert torch.equal(grad[w], want.float()), (w, times)
+        assert bool((base[:32] == 7.0).all()) and bool((base[-32:] == 7.0).all())
+        assert bool((inside[:, :behind] == 7.0).all()) and bool((inside[:, behind + N * K:] == 7.0).all())
+
+
+# ---- large tiles without shares of the rows -----------------------------------------------
+
+@pytest.mark.parametrize("P,rows,N,K,behind,gap", [(1, 513, 4096, 4096, 0, 0), (1, 600, 4090, 3850, 5, 3), (1, 512, 3585, 3841, 32, 0), (2, 2500, 2816, 2816, 0, 64),
+                                                   (4, 2049 * 4, 1800, 2040, 7, 0), (8, 8 * 545, 2000, 2048, 31, 1)])
+def test_large_tiles_without_shares(P, rows, N, K, behind, gap):
+    assert plan("bf16", P, rows, N, K, behind == 0) == ("large", 1)
+    check(P, rows, N, K, "bf16", behind, gap)
+
+
+def test_large_tiles_of_uneven_shares():
+    P, rows, N, K = 4, 2400, 1900, 2048
+    assert plan("bf16", P, rows, N, K, False) == ("large", 1)
+    check(P, rows, N, K, "bf16", 11, 2, [3, 3, 40, 2040, 2399])
+
+
+@pytest.mark.parametrize("P,rows,N,K,shares", [(1, 16384, 1000, 1024, 16), (2, 10000, 1024, 1800, 4), (1, 5000, 2048, 4000, 2)])
+def test_large_tiles_in_shares(P, rows, N, K, shares):
+    assert plan("bf16", P, rows, N, K, False) == ("large", shares)
+    check(P, rows, N, K, "bf16", 3, 1)
