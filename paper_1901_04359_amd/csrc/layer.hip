@@ -123,7 +123,6 @@ constexpr int64_t kGradRowsBig = 512;                               // rows of a
 // Tiles across in a band (tile_at) where products bound the call and L2 has to hold dY and X (in us, 4 / 8 / whole rows: 8192 rows, 4096 x
 // 4096 in fp32, tiles of 128, 803 / 812 / 872).  Whole rows of tiles where writing does, or where two tiles write one memory line.
 constexpr uint32_t kGradBand = 4;
-constexpr int64_t kGradLinesK = 512, kGradLinesRows = 256;         // (rows times the parts of a dY value)
 GradPlan grad_plan_of(bool big, int64_t rows, int32_t P, int64_t N, int64_t K) {
     GradPlan g;
     const int64_t side = big ? 256 : 128;
@@ -153,6 +152,20 @@ GradPlan grad_plan(bool bf16, int64_t rows, int32_t P, int64_t N, int64_t K) {
     const bool gain = large.splits == 1 ? 7 * ((large.jobs + 255) / 256) <= 2 * ((small.jobs + 255) / 256)
                                         : large.jobs >= 192 && (small.splits > 1 || rows / P / large.splits >= 2 * kGradShareRowsBig);
     return gain ? large : small;
+}
+
+// Tiles that begin where memory lines do and write them past the caches (LINES), `aligned`: every row of dW begins with a line; else the last of up to 31
+// more columns.  They need rows of whole lines (K a multiple of 32), and pay where writing bounds the call (rows times the parts of a dY value) and
+// the result is more than the 256 MB of the memory-side cache hold.  (us, without / with LINES, workers x N x K, rows of every worker, in bf16 unless
+// stated.  Aligned: 16 x 2048 x 2048 64: 58 / 51, 256: 100 / 79, 384: 117 / 115; fp32 64: 75 / 69, 86: 85 / 89, 128: 97 / 101; fp16 128: 82 / 81, 192: 95 /
+// 106; 256 x 512 x 512 64: 70 / 54; half of it and less, 8 x 2048 x 2048 64: 29.5 / 29.4, 256: 40 / 42; 8 x 1000 x 4096 64: 30 / 32.
+// Not aligned: 4 x 4096 x 9216 64: 130 / 117, 128: 169 / 138, 384: 266 / 274; 32 x 2048 x 2048 64: 133 / 108, 128: 154 / 136; 64 x 1024 x 1024 64: 67 /
+// 64, 128: 84 / 82, 256: 107 / 117; 512 x 512 x 512 64: 156 / 141, 128: 179 / 184, 256: 217 / 301; 8 x 1000 x 4096 64: 30 / 36; fp32 16 x 4096 x 4096
+// 22: 263 / 222, 43: 302 / 293; 4 x 4096 x 9216 22: 136 / 124, 43: 154 / 162; 16 x 2048 x 2048 22: 64 / 66; fp16 24 x 1000 x 4096 32: 89 / 85, 64: 105 / 109.)
+constexpr int64_t kGradWriteRows = 256;
+bool grad_lines(int parts, int64_t rows_each, int32_t P, int64_t N, int64_t K, bool aligned) {
+    if (K % 32 != 0 || rows_each * parts > kGradWriteRows || P * N < ((1 << 26) + K - 1) / K) return false;
+    return aligned || (parts == 1 ? rows_each <= 128 && K >= 1024 : rows_each * parts <= 64 && K >= 4096);
 }
 
 }  // namespace
@@ -316,13 +329,10 @@ int gtopk_weight_grad(const void* dy, int32_t dtype, int64_t dy_stride, const ui
     const bool split = g.splits > 1;
     float* const to = split ? (float*)ws : grad;
     const int64_t to_stride = split ? g.part_stride : grad_stride, split_stride = split ? g.part_stride * P : 0;
-    // Rows of whole memory lines (K a multiple of 32): tiles that begin where lines do, also in a row that does not, write past
-    // the caches (LINES), the last of up to 31 more columns; where writing bounds the call, and from kGradLinesK on, where the
-    // extra column of tiles is a small part.  (TB/s, 64 rows of every worker, without / with: 4096 x 9216 5.2 / 6.1; 1000 x 4096 4.4
-    // / 5.9; 2048 x 2048 4.3 / 6.3; the shares of 1501 rows by seven random cuts, 1000 x 4096 in fp32: 79 us without, in tiles of 128, 110 with.)
+    const int parts = value_parts(dtype);
     const bool aligned_rows = K % 32 == 0 && to_stride % 32 == 0 && aligned(to, 128);
-    const bool writes = rows / P * (int64_t)value_parts(dtype) <= kGradLinesRows;
-    const bool lines = !g.big && writes && (aligned_rows || (K % 32 == 0 && K >= kGradLinesK && !split));
+    const bool writes = rows / P * parts <= kGradWriteRows;
+    const bool lines = grad_lines(parts, rows / P, P, N, K, aligned_rows);
     // An fp16 or fp32 dY is taken apart once per tile: twice as wide ones, with eight waves, where writing does not bound the call (us, 128 /
     // 256 wide, fp32: 8192 rows, 4096 x 4096 805 / 666; 188 rows of 8 workers, 1000 x 4096 66 / 56; 150 rows of 4, 1000 x 1024 16.3 / 15.2; 200 of 16,
     // 2000 x 128, where half of a tile is empty, 18.6 / 17.8.  bf16, 64 rows of 16 workers, 4096 x 9217: 484 / 505.)

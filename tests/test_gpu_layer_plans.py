@@ -1,4 +1,5 @@
-"""Weight gradients at the sizes that decide which tiles they take: large tiles, without shares of the rows and with.  The rules are written out here as well (`plan`), so that a
+"""Weight gradients at the sizes that decide which tiles they take: results that are written along memory lines, and large tiles, without
+shares of the rows and with.  The rules are written out here as well (`plan`), so that a
 change to them does not silently leave a kernel without its test.
 
 Inputs are small integers, sums are exact in fp32 in every order, and the results are compared to the bit."""
@@ -26,7 +27,7 @@ def tiles_of(side, P, rows, N, K):
 
 
 def plan(dtype, P, rows, N, K, aligned):
-    """(kernel, shares of the rows) that a weight gradient takes, but for results along memory lines"""
+    """(kernel, shares of the rows) that a weight gradient takes; aligned: every row of dW begins with a memory line of 128 bytes"""
     each = rows // P
     small, shares = tiles_of(128, P, rows, N, K)
     if dtype == "bf16" and each >= 512:
@@ -37,6 +38,9 @@ def plan(dtype, P, rows, N, K, aligned):
             gain = large * large_shares >= 192 and (shares > 1 or each // large_shares >= 2048)
         if gain:
             return "large", large_shares
+    if K % 32 == 0 and each * PARTS[dtype] <= 256 and P * N * K >= 2 ** 26:
+        if aligned or (each <= 128 and K >= 1024 if dtype == "bf16" else each * PARTS[dtype] <= 64 and K >= 4096):
+            return "lines", shares
     return ("small" if dtype == "bf16" else "wide"), shares
 
 
@@ -77,6 +81,28 @@ def check(P, rows, N, K, dtype, behind, gap, begin=None, again=True):
             assert torch.equal(grad[w], want.float()), (w, times)
         assert bool((base[:32] == 7.0).all()) and bool((base[-32:] == 7.0).all())
         assert bool((inside[:, :behind] == 7.0).all()) and bool((inside[:, behind + N * K:] == 7.0).all())
+
+
+# ---- results written along memory lines -------------------------------------------------
+
+@pytest.mark.parametrize("P,T,N,K,behind,gap", [
+    (64, 45, 1021, 1056, 0, 0), (64, 45, 1021, 1056, 1, 0), (64, 30, 1021, 1056, 31, 1), (63, 33, 1021, 1152, 7, 25), (3, 100, 5500, 4128, 16, 8),
+    (2, 3, 8200, 4224, 30, 3), (1, 64, 16400, 4096, 100, 28), (1024, 2, 64, 1024, 5, 0), (260, 17, 512, 512, 0, 0), (3000, 1, 700, 32, 32, 64)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_large_results_wherever_rows_begin(P, T, N, K, behind, gap, dtype):
+    aligned = behind % 32 == 0 and (behind + N * K + gap) % 32 == 0
+    few = T * PARTS[dtype] <= 64
+    expected = "lines" if T * PARTS[dtype] <= 256 and (aligned or (K >= 1024 if dtype == "bf16" else few and K >= 4096)) else None
+    assert (plan(dtype, P, P * T, N, K, aligned)[0] == "lines") == (expected == "lines")
+    check(P, P * T, N, K, dtype, behind, gap)
+
+
+def test_large_result_of_uneven_shares():
+    """One worker without rows, one with most of them, some rows that nobody has: along lines from an odd place."""
+    P, rows, N, K = 16, 640, 1100, 4096
+    begin = [0, 0, 5, 400, 400] + [400 + 17 * i for i in range(1, 13)]
+    assert plan("bf16", P, rows, N, K, False)[0] == "lines"
+    check(P, rows, N, K, "bf16", 9, 3, begin)
 
 
 # ---- large tiles without shares of the rows -----------------------------------------------
