@@ -120,8 +120,10 @@ struct GradPlan {
 constexpr uint64_t kMaxJobs = 0x3FFFFFFF;
 constexpr int64_t kGradShareRows = 256, kGradShareRowsBig = 1024;   // rows of a share, at least
 constexpr int64_t kGradRowsBig = 512;                               // rows of a worker from which on large tiles are weighed
-// Tiles across in a band (tile_at) where products bound the call and L2 has to hold dY and X (in us, 4 / 8 / whole rows: 8192 rows, 4096 x
-// 4096 in fp32, tiles of 128, 803 / 812 / 872).  Whole rows of tiles where writing does, or where two tiles write one memory line.
+// Tiles across in a band (tile_at) where products bound the call and L2 has to hold dY and X.  Whole rows of tiles where writing does, or
+// where two tiles write one memory line.  (us, 2 / 4 / 8 / 16 / whole rows.  fp32, tiles of 128 x 256: 8192 rows, 8192 x 8192 2877 / 2818 / 2810 / 2831 /
+// 2879; four workers of 2048 rows, 4096 x 4096 747 / 730 / 752 / 754 / 758.  bf16, large tiles, the same two: 1005 / 984 / 972 / 961 / 973; 292 / 273 /
+// 285 / 286 / 284.)
 constexpr uint32_t kGradBand = 4;
 GradPlan grad_plan_of(bool big, int64_t rows, int32_t P, int64_t N, int64_t K) {
     GradPlan g;
@@ -334,8 +336,9 @@ int gtopk_weight_grad(const void* dy, int32_t dtype, int64_t dy_stride, const ui
     const bool writes = rows / P * parts <= kGradWriteRows;
     const bool lines = grad_lines(parts, rows / P, P, N, K, aligned_rows);
     // An fp16 or fp32 dY is taken apart once per tile: twice as wide ones, with eight waves, where writing does not bound the call (us, 128 /
-    // 256 wide, fp32: 8192 rows, 4096 x 4096 805 / 666; 188 rows of 8 workers, 1000 x 4096 66 / 56; 150 rows of 4, 1000 x 1024 16.3 / 15.2; 200 of 16,
-    // 2000 x 128, where half of a tile is empty, 18.6 / 17.8.  bf16, 64 rows of 16 workers, 4096 x 9217: 484 / 505.)
+    // 256 wide, fp32 and fp16: 8192 rows, 4096 x 4096 821 / 679 and 614 / 503; 188 rows of 8 workers, 1000 x 4096 66 / 56 and 57 / 51; 150 rows of 4, 1000 x
+    // 1024 15.5 / 14.0 and 13.9 / 12.5; 200 of 16, 2000 x 128, where half of a tile is empty, 18.9 / 18.3 and 16.5 / 15.6; 64 of 16, 4096 x 9217 637 / 647 and
+    // 615 / 577; 64 of 32, 128 x 128 7.6 / 7.8 and 7.1 / 7.3.  bf16, 64 rows of 16 workers, 4096 x 9217: 484 / 505.)
     const bool wide = !lines && dtype != GTOPK_BF16;
     const uint32_t tiles_k = wide ? (uint32_t)ceil_div(K, 256) : lines && !aligned_rows ? (uint32_t)ceil_div(K + 31, 128) : g.tiles_k;
     const uint32_t jobs = g.tiles_n * tiles_k * (uint32_t)P * g.splits, band = writes || !aligned_rows ? tiles_k : kGradBand;

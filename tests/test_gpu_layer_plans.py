@@ -1,5 +1,5 @@
-"""Weight gradients at the sizes that decide which tiles they take: results that are written along memory lines, and large tiles, without
-shares of the rows and with.  The rules are written out here as well (`plan`), so that a
+"""Weight gradients at the sizes that decide which tiles they take: results that are written along memory lines, large tiles without shares
+of the rows, bands of tiles, and sums over most of a long batch.  The rules are written out here as well (`plan`), so that a
 change to them does not silently leave a kernel without its test.
 
 Inputs are small integers, sums are exact in fp32 in every order, and the results are compared to the bit."""
@@ -124,3 +124,44 @@ def test_large_tiles_of_uneven_shares():
 def test_large_tiles_in_shares(P, rows, N, K, shares):
     assert plan("bf16", P, rows, N, K, False) == ("large", shares)
     check(P, rows, N, K, "bf16", 3, 1)
+
+
+# ---- bands of tiles, and long sums --------------------------------------------------------
+
+@pytest.mark.parametrize("P,rows,N,K", [(1, 300, 300, 2336), (2, 800, 520, 1312), (3, 1100, 130, 4096)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_bands_of_tiles(P, rows, N, K, dtype):
+    """More than four tiles across and several down, aligned rows, enough rows that writing does not bound the call: tiles in bands of four."""
+    each = rows // P
+    kernel, shares = plan(dtype, P, rows, N, K, True)
+    assert each * PARTS[dtype] > 256 and cdiv(K, 256 if kernel == "wide" else 128) > 4 and N > 128 and kernel in ("small", "wide")
+    begin = None if rows % P == 0 else [0, 100, 101, rows]
+    check(P, rows, N, K, dtype, 0, 0, begin)
+
+
+def test_a_sum_over_most_of_a_batch_past_32_bits():
+    """Codes of more than 2^32 bytes, of which one worker has all but a few rows: its sum of half a million rows, in the first and the last columns."""
+    import torch
+    from paper_1901_04359_amd import binding as B
+    rows, N, K, tail = 560_000, 12, 8192, 130
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(11)
+    table = torch.from_numpy(ref.encode(np.arange(-2.0, 3.0))).cuda()
+    codes = torch.empty(rows, K, dtype=torch.uint8, device="cuda")
+    for at in range(0, rows, 70_000):
+        codes[at:at + 70_000] = table[torch.randint(0, 5, (70_000, K), device="cuda", generator=gen, dtype=torch.uint8).int()]
+    assert codes.numel() > 2 ** 32
+    scales = torch.full((rows, 64), 127, dtype=torch.uint8, device="cuda")
+    dy = torch.randint(-2, 3, (rows, N), device="cuda", generator=gen, dtype=torch.int32)
+    begin = [0, 100, rows - tail, rows]
+    plan_ = torch.tensor(begin, dtype=torch.int32, device="cuda")
+    for dtype in TYPES:
+        grad = torch.empty(3, N, K, device="cuda")
+        say(f"layer: weight_grad {dtype} of a batch past 2^32 bytes")
+        B.gtopk_weight_grad(dy.to(torch_type(dtype)), codes, scales, plan_, grad, False, B.alloc_weight_grad_workspace(rows, 3, N, K))
+        for cols in (slice(0, 128), slice(4000, 4128), slice(K - 128, K)):
+            x = codes[:, cols].contiguous().view(torch.float8_e4m3fn).double()
+            for w in range(3):
+                want = dy[begin[w]:begin[w + 1]].double().t().contiguous() @ x[begin[w]:begin[w + 1]]
+                assert float(want.abs().max()) < 2 ** 24
+                assert torch.equal(grad[w, :, cols].double(), want), (w, cols)
