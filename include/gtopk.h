@@ -266,7 +266,7 @@ int gtopk_dense_topk(const float* dense, int64_t m, int32_t k, uint32_t* g_idx, 
  *   The value of a code c in a block of scale s is e4m3(c) * 2^(s - 127).  codes is 16-byte aligned, scales 4-byte.
  *   A magnitude of 2^128 or more (scales from 247 on; the pack calls make one, 2^128, of a finite value from 1.9375 * 2^127 on)
  *   is more than fp32 holds: gtopk_unpack and gtopk_activation_grad take it as an infinity, with f and f' what they tend to
- *   there; so do products to fp32 and weight gradients (a 16-bit result of a product takes it as it is).
+ *   there, and gtopk_weight_grad too; gtopk_scaled_product takes it as it is.
  * Dense matrices (x, dy, out, dx, grad) have contiguous rows at any stride >= their columns and need the
  * alignment of one value only, as a layer may lie anywhere in a flat row.  dtype is one of gtopk_dtype.
  * Sizes: rows and columns 1 .. 2^31 - 1; rows (M of the product) may also be 0: then there is nothing to
@@ -321,9 +321,8 @@ int gtopk_activation_grad(const uint8_t* codes, int64_t code_stride, const uint8
  * out = A B^T for packed A (M x K) and packed B (N x K): out[m][n] = sum over k of A[m][k] * B[n][k], rounded once to
  * dtype.  Forward pass of a layer: A its packed input, B its packed weights; input gradient: A the packed output
  * gradient, B the transposed packed weights.
- *   GTOPK_F32:  products of values below 2^128 are exact, sums are fp32 (values below 2^-126 may be rounded to a multiple of
- *               2^-133).
- *   GTOPK_BF16, GTOPK_F16: twice as fast.  The eight products of k = 8 j .. 8 j + 7 are exact, but each is cut
+ *   GTOPK_F32:  products are exact, sums are fp32 (values below 2^-126 may be rounded to a multiple of 2^-133).
+ *   GTOPK_BF16, GTOPK_F16: up to twice as fast.  The eight products of k = 8 j .. 8 j + 7 are exact, but each is cut
  *               off at 2^-13 of the largest of the eight (its leading bit); all further sums are fp32.
  *   Strides of codes and scales (and so K) of at most 2^23; fewer than 2^24 tiles of 128 x 128 in out, for M <= 32
  *   N of at most 2^26.

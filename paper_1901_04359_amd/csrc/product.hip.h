@@ -81,6 +81,35 @@ __device__ __forceinline__ floatx4 multiply(const Operand<EXACT>& b, const Opera
     }
 }
 
+// With a scale from 247 on a value may be 2^128 or more, which decodes to a bf16 infinity; a sum that it enters is not finite.  Such sums are computed
+// once more with the scales of both rows applied together, to products of the bare codes, one block of 128 after the other as
+// it lies in memory.  This adds one; 32 codes per lane at a and b, their rows' scales at a_scale and b_scale.  (A lane's four results are of B's
+// rows 4 quarter .. 4 quarter + 3, whose scales lanes of those numbers have.)
+// (`none` stays 0 while all values are finite: one operation each)
+__device__ __forceinline__ void note_lost(float& none, floatx4 v) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) none = fmaf(v[r], 0.0f, none);
+}
+__device__ __forceinline__ intx8 codes_at(const uint8_t* p) {
+    const intx4 lo = *reinterpret_cast<const intx4*>(p), hi = *reinterpret_cast<const intx4*>(p + 16);
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+__device__ __forceinline__ floatx4 add_far(const uint8_t* b, uint32_t b_scale, const uint8_t* a, uint32_t a_scale, floatx4 sum) {
+    const floatx4 part = multiply<true>(prepare<true>(codes_at(b), 127u), prepare<true>(codes_at(a), 127u), floatx4{});
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const uint32_t of_b = (uint32_t)__shfl((int)b_scale, (int)(lane_id() / 16 * 4) + r);
+        sum[r] += a_scale == 255u || of_b == 255u ? __uint_as_float(0x7FC00000u) : __builtin_ldexpf(part[r], (int)(a_scale + of_b) - 254);
+    }
+    return sum;
+}
+// v, with those of its values that are not finite taken from `again`
+__device__ __forceinline__ floatx4 mended(floatx4 v, floatx4 again) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) v[r] = finite_bits(__float_as_uint(v[r])) ? v[r] : again[r];
+    return v;
+}
+
 // A block computes BM x BN values with BM/WM x BN/WN waves of WM x WN each.  A block of 128 of the tile's rows of A and B
 // goes straight from global memory into one of two LDS buffers while the matrix instructions work on the other; the scales
 // of four blocks go together (a word per row: fetched one by one they would be as many requests as the codes).
@@ -222,14 +251,38 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * kWave, 1) void k_product(
         if (kb + 3 < nb) block(kb + 3, 3, s_codes1, s_codes0);
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // the last loads into LDS, which nobody reads, end before the block does
+    float none = 0.0f;
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
         const int64_t m = m0 + wm + i * 16 + in16;
-        if (m >= M) continue;
 #pragma unroll
         for (int j = 0; j < TN; ++j) {
             const int64_t n = n0 + wn + j * 16 + quarter * 4;
-            if (n < N) store4<D>(out + m * out_stride + n, N - n, sum[i][j]);
+            if constexpr (EXACT) note_lost(none, sum[i][j]);
+            if (m < M && n < N) store4<D>(out + m * out_stride + n, N - n, sum[i][j]);
+        }
+    }
+    if constexpr (EXACT) {
+        if (!__ballot(none != 0.0f)) return;
+        // (an infinity or a NaN: each subtile again, if a scale of its rows may be the cause)
+        for (int t = 0; t < TM * TN; ++t) {
+            const uint32_t row_a = wm + t / TN * 16 + in16, row_b = wn + t % TN * 16 + in16;
+            const uint32_t ra = row_a < a_last ? row_a : a_last, rb = row_b < b_last ? row_b : b_last;
+            const uint8_t *pa = a_base + (int64_t)ra * a.code_stride + quarter * 32, *pb = b_base + (int64_t)rb * b.code_stride + quarter * 32;
+            const uint8_t *qa = a.scales + (m0 + ra) * a.scale_stride + first, *qb = b.scales + (n0 + rb) * b.scale_stride + first;
+            bool far = false;
+            for (uint32_t kb = quarter; kb < nb; kb += 4) far = far || (qa[kb] >= 247u && qa[kb] != 255u) || (qb[kb] >= 247u && qb[kb] != 255u);
+            if (!__ballot(far)) continue;
+            floatx4 again = {};
+            for (uint32_t kb = 0; kb < nb; ++kb) again = add_far(pb + (uint64_t)kb * kPackBlock, qb[kb], pa + (uint64_t)kb * kPackBlock, qa[kb], again);
+            const int64_t m = m0 + row_a, n = n0 + wn + t % TN * 16 + quarter * 4;
+            if (m < M && n < N) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    typename D::T* const p = out + m * out_stride + n + r;
+                    if (n + r < N && !finite_bits(__float_as_uint((float)*p))) *p = (typename D::T)again[r];
+                }
+            }
         }
     }
 }
@@ -258,10 +311,6 @@ __global__ __launch_bounds__(kThinWaves * kWave) void k_product_thin(PackedMatri
         a_row[i] = a.codes + m * a.code_stride + quarter * 32;
         a_scale[i] = a.scales + m * a.scale_stride;
     }
-    auto codes = [](const uint8_t* p) {
-        const intx4 lo = *reinterpret_cast<const intx4*>(p), hi = *reinterpret_cast<const intx4*>(p + 16);
-        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-    };
     floatx4 sum[TM] = {};
     for (uint32_t k0 = wave; k0 < nb; k0 += kThinWaves * kAhead) {
         intx8 va[kAhead][TM], vb[kAhead];
@@ -269,11 +318,11 @@ __global__ __launch_bounds__(kThinWaves * kWave) void k_product_thin(PackedMatri
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {         // behind the last block the last one once more, which is not used
             const uint32_t kb = k0 + u * kThinWaves < nb ? k0 + u * kThinWaves : nb - 1;
-            vb[u] = codes(b_row + (uint64_t)kb * kPackBlock);
+            vb[u] = codes_at(b_row + (uint64_t)kb * kPackBlock);
             sb[u] = b_scale[kb];
 #pragma unroll
             for (int i = 0; i < TM; ++i) {
-                va[u][i] = codes(a_row[i] + (uint64_t)kb * kPackBlock);
+                va[u][i] = codes_at(a_row[i] + (uint64_t)kb * kPackBlock);
                 sa[u][i] = a_scale[i][kb];
             }
         }
@@ -286,7 +335,17 @@ __global__ __launch_bounds__(kThinWaves * kWave) void k_product_thin(PackedMatri
         }
     }
 #pragma unroll
-    for (int i = 0; i < TM; ++i) s_sum[wave][i][lane] = sum[i];
+    for (int i = 0; i < TM; ++i) {
+        float none = 0.0f;
+        note_lost(none, sum[i]);
+        if (kExact && __ballot(none != 0.0f)) {
+            floatx4 again = {};
+            for (uint32_t kb = wave; kb < nb; kb += kThinWaves)
+                again = add_far(b_row + (uint64_t)kb * kPackBlock, b_scale[kb], a_row[i] + (uint64_t)kb * kPackBlock, a_scale[i][kb], again);
+            sum[i] = mended(sum[i], again);
+        }
+        s_sum[wave][i][lane] = sum[i];
+    }
     __syncthreads();
     for (int i = wave; i < TM; i += kThinWaves) {
         floatx4 v = s_sum[0][i][lane];

@@ -138,10 +138,10 @@ def test_product_of_every_scale_that_pack_makes(M, N, K, dtype, unit):
     assert torch.equal(turned.cpu(), want.T.float().to(t))
 
 
-@pytest.mark.parametrize("M,N,K", [(3, 40, 300), (70, 150, 2500), (2817, 2850, 300)])
+@pytest.mark.parametrize("M,N,K", [(3, 40, 300), (20, 33, 3000), (70, 150, 2500), (200, 4097, 1030), (2817, 2850, 300)])
 def test_product_of_values_that_fp32_cannot_hold(M, N, K):
-    """In row 1 of A stand 2^128 and -2^128 with products of 2^108 and -2^108: a 16-bit result takes them as they are (if it
-    can hold them), an fp32 result as infinities.  All other rows are as they were."""
+    """In rows 1 and 2 of A stand 2^128 and -2^128, with products of 2^108 and -2^108, and in B's last row a NaN: values count as
+    they are, in every type that can hold the result."""
     import torch
     from paper_1901_04359_amd import binding as B
     a, b = int_codes(M, K, 3), np.abs(int_codes(N, K, 4))
@@ -152,17 +152,18 @@ def test_product_of_values_that_fp32_cannot_hold(M, N, K):
     a[1, 5] = 0x78                           # 256 * 2^120
     a[2, :], sa[2, :] = 0, 247
     a[2, K - 1] = 0xF8
+    b[N - 1, K - 2] = 0x7F
+    b[N - 2, (nb - 1) * 128:], sb[N - 2, nb - 1] = 0, 254     # zeros at the largest scale
     want = torch.from_numpy(ref.values(a, sa, K) @ ref.values(b, sb, K).T)
-    assert bool((want[1] == 2.0 ** 108).all()) and bool((want[2] == -2.0 ** 108).all())
+    assert bool((want[1, :N - 2] == 2.0 ** 108).all()) and bool((want[2, :N - 2] == -2.0 ** 108).all())
     say(f"layer: product {M}x{N}x{K} of 2^128")
     for dtype in TYPES:
         t = torch_type(dtype)
         out = torch.zeros(M, N, dtype=t, device="cuda")
         B.gtopk_scaled_product(*packed_on_gpu(a, sa), *packed_on_gpu(b, sb), K, out, B.alloc_product_workspace(M, N, K))
-        w = want.float().to(t)
-        if dtype == "f32":
-            w[1], w[2] = math.inf, -math.inf
-        assert torch.equal(out.cpu(), w)
+        w, got = want.float().to(t), out.cpu()
+        assert torch.equal(torch.isnan(got), torch.isnan(w)) and int(torch.isnan(w).sum()) == M
+        assert torch.equal(torch.nan_to_num(got), torch.nan_to_num(w))
 
 
 @pytest.mark.parametrize("M,N,K", [(3, 40, 300), (20, 40, 300), (130, 140, 300), (2817, 2850, 300)])
