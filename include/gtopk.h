@@ -321,8 +321,9 @@ int gtopk_activation_grad(const uint8_t* codes, int64_t code_stride, const uint8
  * out = A B^T for packed A (M x K) and packed B (N x K): out[m][n] = sum over k of A[m][k] * B[n][k], rounded once to
  * dtype.  Forward pass of a layer: A its packed input, B its packed weights; input gradient: A the packed output
  * gradient, B the transposed packed weights.
- *   GTOPK_F32:  products are exact, sums are fp32 (values below 2^-126 may be rounded to a multiple of 2^-133).
- *   GTOPK_BF16, GTOPK_F16: up to twice as fast.  The eight products of k = 8 j .. 8 j + 7 are exact, but each is cut
+ *   GTOPK_F32, and all types for M <= 32:  products are exact, sums are fp32 (values below 2^-126 may be rounded to a multiple
+ *               of 2^-133).
+ *   GTOPK_BF16, GTOPK_F16 for M > 32: up to twice as fast.  The eight products of k = 8 j .. 8 j + 7 are exact, but each is cut
  *               off at 2^-13 of the largest of the eight (its leading bit); all further sums are fp32.
  *   Strides of codes and scales (and so K) of at most 2^23; fewer than 2^24 tiles of 128 x 128 in out, for M <= 32
  *   N of at most 2^26.

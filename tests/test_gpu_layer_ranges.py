@@ -9,7 +9,7 @@ import pytest
 
 from tests import layer_reference as ref
 from tests.gpu_harness import say
-from tests.test_gpu_layer import TYPES, half_step, packed_on_gpu, torch_type
+from tests.test_gpu_layer import TYPES, half_step, packed_on_gpu, torch_type, values_in
 
 pytestmark = pytest.mark.gpu
 
@@ -260,3 +260,24 @@ def test_weight_grad_of_values_at_both_ends(dtype, P, rows, N, K):
     assert np.array_equal(fine, np.repeat(~far[:, None, :], N, axis=1))
     want, size = ref.weight_grad(dy, np.where(np.repeat(far, each, axis=0), 0.0, x), begin), ref.weight_grad(dy, np.abs(x), begin)
     assert (np.abs(got - want)[fine] <= ((each + 4) * 2.0 ** -23 * size)[fine]).all()
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("M,N,K", [(1, 300, 5000), (16, 130, 1000), (17, 90, 2050), (32, 300, 4096)])
+def test_product_of_few_rows_holds_fp32_sums(M, N, K, dtype):
+    """Reading B bounds these, whatever the products: a 16-bit result is the fp32 sum, off by at most (K + 4) 2^-23 of the magnitudes, rounded
+    once, also where the sum cancels."""
+    import torch
+    from paper_1901_04359_amd import binding as B
+    t = torch_type(dtype)
+    a, b = ref.pack(values_in(M, K, 41)), ref.pack(values_in(N, K, 42) / math.sqrt(K), tiles=True)
+    va, vb = ref.values(*a, K), ref.values(*b, K)
+    out = torch.zeros(M, N, dtype=t, device="cuda")
+    say(f"layer: product {M}x{N}x{K} to {dtype}, fp32 sums")
+    B.gtopk_scaled_product(*packed_on_gpu(*a), *packed_on_gpu(*b), K, out, B.alloc_product_workspace(M, N, K))
+    want, bound = va @ vb.T, (K + 4) * 2.0 ** -23 * (np.abs(va) @ np.abs(vb).T)
+    err = np.abs(out.double().cpu().numpy() - want)
+    assert (err <= bound * (1 + half_step(t)) + half_step(t) * np.abs(want) + (2.0 ** -25 if dtype == "f16" else 0.0)).all()
+    # in norm such sums are off by 2^-17 of the results at most, 2^-6 of fp16's smallest step of 2^-11: nearly every result is
+    # the nearest number of its type (twice 2^-6 for results that are smaller than most)
+    nearest = torch.from_numpy(want).to(t)
+    assert float((out.cpu() == nearest).double().mean()) > 1 - 2 * 2.0 ** -6
