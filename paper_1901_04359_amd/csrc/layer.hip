@@ -77,7 +77,7 @@ struct ProductPlan {
     uint32_t tiles_m, tiles_n, share, shares;       // blocks of 128 per share
     int64_t stride;                                 // of a share's result
 };
-// (us, without tiles / with: 32 x 4096 x 9216 15.1 / 15.5; 17 rows 12.9 / 15.0; 64 rows 24.6 / 16.9)
+// (us, without tiles / with, where 16-bit results lose bits: 32 x 4096 x 9216 16.1 / 15.5; 17 rows 12.9 / 15.0; 64 rows 24.6 / 16.9)
 constexpr int64_t kThinRows = 32;
 // blocks of 128 per share, at least; a multiple of 4.  (us with 4, 8, 16: 128 x 4096 x 4096 17.5, 15.2, 17.6; 1024^3 12.7, 9.2, 9.2;
 // 64 x 4096 x 9216 16.9, 16.9, 22.1; 512 x 1000 x 4096 16.2, 15.5, 17.4, and 22.9 in one piece)

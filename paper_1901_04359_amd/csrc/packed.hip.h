@@ -8,7 +8,8 @@
 // which buys a floating-point code less than one binade of its 15 at the small end and nothing else, and
 // would cost a multiply per product and block; a power of two goes into the matrix instruction as its scale operand.
 //
-// Every kernel here moves each byte once and is bound by HBM bandwidth.
+// Every kernel here moves each byte once and is bound by HBM bandwidth, but for tanh and GELU from 8 bits to 16, which arithmetic bounds (unpack of 8192 x 4096:
+// none and ReLU 17 us, logistic and SiLU 18, tanh 24, GELU 25; activation gradients 26, of GELU 30).
 #pragma once
 #include "common.hip.h"
 

@@ -83,15 +83,16 @@ __device__ __forceinline__ floatx4 multiply(const Operand<EXACT>& b, const Opera
     }
 }
 
-// With a scale from 247 on a value may be 2^128 or more, which decodes to a bf16 infinity; a sum that it enters is not finite.  Such sums are computed
-// once more with the scales of both rows applied together, to products of the bare codes, one block of 128 after the other as
-// it lies in memory.  This adds one; 32 codes per lane at a and b, their rows' scales at a_scale and b_scale.  (A lane's four results are of B's
-// rows 4 quarter .. 4 quarter + 3, whose scales lanes of those numbers have.)
-// (`none` stays 0 while all values are finite: one operation each)
+// `none` stays 0 while all values are finite: one operation each
 __device__ __forceinline__ void note_lost(float& none, floatx4 v) {
 #pragma unroll
     for (int r = 0; r < 4; ++r) none = fmaf(v[r], 0.0f, none);
 }
+// With a scale from 247 on a value may be 2^128 or more, which decodes to a bf16 infinity; a sum that it enters is not finite.  Such sums are computed
+// once more with the scales of both rows applied together, to products of the bare codes, one block of 128 after the other as
+// it lies in memory (2048 x 4096 x 9216 to fp32: a NaN in one row of A costs the look at the scales, 202 us instead of 150, such a scale there 390).  This adds
+// one; 32 codes per lane at a and b, their rows' scales at a_scale and b_scale.  (A lane's four results are of B's
+// rows 4 quarter .. 4 quarter + 3, whose scales lanes of those numbers have.)
 __device__ __forceinline__ intx8 codes_at(const uint8_t* p) {
     const intx4 lo = *reinterpret_cast<const intx4*>(p), hi = *reinterpret_cast<const intx4*>(p + 16);
     return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
@@ -115,10 +116,11 @@ __device__ __forceinline__ floatx4 mended(floatx4 v, floatx4 again) {
 // A block computes BM x BN values with BM/WM x BN/WN waves of WM x WN each.  A block of 128 of the tile's rows of A and B
 // goes straight from global memory into one of two LDS buffers while the matrix instructions work on the other; the scales
 // of four blocks go together (a word per row: fetched one by one they would be as many requests as the codes).
-// Tiles of 128 x 128 with four waves, two blocks per compute unit: 2048 x 4096 x 9216 to bf16 in 77 us = 2.0 PFLOP/s, 8192^3 in 509; to
-// fp32 147 and 929.  What bounds them is the way into LDS: of 8192^3's 509 us the loads alone take 407, the matrix instructions
-// alone 282, all but the loads 337.  Tiles of 256 x 256 with eight waves, one block per compute unit, need half the loads: 409 us = 2.7 PFLOP/s,
-// to fp32 773 = 1.4 (the matrix instructions of either type at 0.87 of what a library product of 8192^3 reaches).  Their waves read
+// Tiles of 128 x 128 with four waves, two blocks per compute unit: 2048 x 4096 x 9216 to bf16 in 72 to 79 us = 2.0 to 2.1 PFLOP/s, 8192^3 in 509; to
+// fp32 142 to 149 and 929.  What bounds them is the way into LDS: of 8192^3's 509 us the loads alone take 407, the matrix instructions
+// alone 282, all but the loads 337.  Tiles of 256 x 256 with eight waves, one block per compute unit, need half the loads: 409 to 419 us = 2.6 to 2.7
+// PFLOP/s, to fp32 773 to 792 = 1.4 (the matrix instructions of either type at 0.87 of what a library product of 8192^3 reaches).  (Calls in a row on the
+// same buffers; by turns on buffers that no cache holds, 8192^3 447 and 786 us, 2048 x 4096 x 9216 92 and 146.)  Their waves read
 // A 16 rows at a time, for the registers (kStream).  Slower: 256 x 128 with eight waves 80 us for the first size, with three LDS buffers
 // 81; 256 x 256 with four waves 493 us for 8192^3; decoding B's rows for fp32 once per half block of A's 187 us for the first
 // size, nothing gained with large tiles.
@@ -289,8 +291,8 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * kWave, 1) void k_product(
     }
 }
 
-// Few rows of A (at most 16 TM): what counts is reading B once at the memory's rate (1 x 4096 x 9216: 38 MB in 9.5 us with the host's
-// part of the call; 1 x 16384 x 9216: 151 MB in 29.5 us = 5.1 TB/s).  A block computes 16 columns of C
+// Few rows of A (at most 16 TM): what counts is reading B once at the memory's rate (1 x 4096 x 9216: 38 MB in 9.1 to 9.8 us with the host's
+// part of the call; 1 x 16384 x 9216: 151 MB in 30 us = 5.0 TB/s).  A block computes 16 columns of C
 // with kThinWaves waves that share out the blocks of 128 among them and read both matrices straight into registers, kThinAhead
 // blocks of 128 at a time, so that a compute unit has some 64 KB of B under way; the waves' sums are joined in LDS, in their order.
 constexpr int kThinWaves = 8;
