@@ -126,6 +126,52 @@ def test_large_tiles_in_shares(P, rows, N, K, shares):
     check(P, rows, N, K, "bf16", 3, 1)
 
 
+# ---- scales from the smallest on, and NaN, in the kernels that only large sizes take --------
+
+@pytest.mark.parametrize("kernel,P,rows,N,K,behind", [("lines", 64, 2560, 1021, 1056, 1), ("lines", 64, 1280, 1021, 1056, 0), ("large", 1, 600, 4090, 3850, 5),
+                                                      ("large", 1, 16384, 1000, 1024, 0)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_every_scale_and_nan(kernel, P, rows, N, K, behind, dtype):
+    """X's scales from 1 to 247, a row of dY as far from 1 as X's is on the other side: sums of small integers.  Then a NaN scale and a NaN code,
+    which reach their columns of their worker's gradient and nothing else."""
+    import torch
+    from paper_1901_04359_amd import binding as B
+    each = rows // P
+    if dtype == "f32" and kernel == "lines" and behind == 0:
+        assert plan(dtype, P, rows, N, K, True)[0] == "lines"
+    if dtype == "bf16":
+        assert plan(dtype, P, rows, N, K, behind == 0 and N * K % 32 == 0)[0] == kernel
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(rows + K)
+    per_row = torch.randint(1, 248, (rows, 1), device="cuda", generator=gen, dtype=torch.int32)
+    per_row[0], per_row[1] = 1, 247
+    d = torch.randint(-2, 3, (rows, N), device="cuda", generator=gen, dtype=torch.int32).double()
+    dy = (d * torch.exp2(127.0 - per_row.double())).to(torch_type(dtype))
+    x = torch.randint(-2, 3, (rows, K), device="cuda", generator=gen, dtype=torch.int64)
+    nb = cdiv(K, 128)
+    codes = torch.zeros(rows, nb * 128, dtype=torch.uint8, device="cuda")
+    codes[:, :K] = torch.from_numpy(ref.encode(np.arange(-2.0, 3.0))).cuda()[x + 2]
+    scales = per_row.to(torch.uint8).expand(rows, cdiv(nb, 4) * 4).contiguous()
+    grads = torch.empty(P, behind + N * K, device="cuda")
+    grad = grads[:, behind:].unflatten(1, (N, K))
+    ws = B.alloc_weight_grad_workspace(rows, P, N, K)
+    say(f"layer: weight_grad {dtype} P {P} rows {rows} {N}x{K}, every scale")
+    B.gtopk_weight_grad(dy, codes, scales, None, grad, False, ws)
+    want = [(d[w * each:(w + 1) * each].t().contiguous() @ x[w * each:(w + 1) * each].double()).float() for w in range(P)]
+    for w in range(P):
+        assert torch.equal(grad[w], want[w]), w
+    last, t = P - 1, rows - 2
+    scales[t, 2] = 255
+    codes[t + 1, 7] = 0xFF
+    B.gtopk_weight_grad(dy, codes, scales, None, grad, False, ws)
+    gone = torch.zeros(K, dtype=torch.bool, device="cuda")
+    gone[256:384], gone[7] = True, True
+    for w in range(P):
+        lost = torch.isnan(grad[w])
+        assert torch.equal(lost, (gone & (w == last))[None, :].expand(N, K))
+        assert torch.equal(grad[w][~lost], want[w][~lost])
+
+
 # ---- bands of tiles, and long sums --------------------------------------------------------
 
 @pytest.mark.parametrize("P,rows,N,K", [(1, 300, 300, 2336), (2, 800, 520, 1312), (3, 1100, 130, 4096)])

@@ -193,7 +193,7 @@ def power_rows(rows, N, scales, seed):
     return r.integers(-2, 3, (rows, N)) * np.exp2(127.0 - scales.astype(np.float64))[:, None]
 
 
-# (tiles of 128, also along memory lines, of 128 x 256 and of 256; in one piece and in shares of the rows)
+# (tiles of 128 and of 128 x 256, in one piece and in shares of the rows; the other kernels: test_gpu_layer_plans.py)
 @pytest.mark.parametrize("P,rows,N,K", [(2, 60, 33, 200), (2, 60, 40, 640), (1, 3000, 40, 300), (1, 2000, 1030, 1030), (3, 900, 130, 700)])
 @pytest.mark.parametrize("dtype,low,high", [("f32", 1, 247), ("bf16", 1, 247), ("f16", 114, 140)])
 @pytest.mark.parametrize("unit", [1.0, 64.0])
